@@ -325,6 +325,94 @@ int lc_append(lc_index* idx, void* K, void* V, const int64_t kv_strides[3],
               const void* k_new, const void* v_new, const uint8_t* close_chunk,
               void* ws /* unused, may be NULL */, size_t ws_bytes, void* stream);
 
+/*
+ * A cache in 4 bits.  A row of 128 values takes LC_CACHE4_ROW = 68 bytes instead of bfloat16's 256:
+ *   bytes 0..63    e2m1 codes, value 2 i in the low half of byte i: a sign bit, then 0, .5, 1, 1.5, 2, 3, 4 or 6
+ *   bytes 64..67   for each 32 values an e8m0 byte s: they are multiples of 2^(s - 127); 255: they are no numbers
+ * K4 and V4 are [B][H_kv][tokens] of such rows, addressed through BYTE strides {sequence, head, token}, each a multiple of 4, the
+ * rows 4-byte aligned, one (sequence, head) slab spanning less than 2 GiB.  The index over such a cache is any lc_index: built
+ * from the prompt's bfloat16 keys before they are dropped (lc_build_index, then lc_cache4_store), or from the rows as the
+ * cache holds them (lc_cache4_load, then lc_build_index), grown by lc_append4.  lc_retrieve reads the index alone.
+ * With an index over the bfloat16 keys the bound of Eq. 2 is on their logits, not on those of the rounded rows.
+ */
+#define LC_CACHE4_ROW 68
+
+/*
+ * lc_cache4_store -- rows of keys and values from bfloat16 into a 4-bit cache: row i of K and V, i < counts[b], into row
+ * first[b] + i of K4 and V4.  A block's power of two is the smallest at which its largest value is rounded by no more than
+ * half a step; codes are rounded to the nearest, ties to the even code.  A block with an infinity or a not-a-number
+ * becomes 32 not-a-numbers; finite values stay finite (with s = 253 the code of 4 would be an infinity: 3 stands in).
+ *   first    host int32[B], or NULL for zeros
+ *   counts   host int32[B]; rows behind the range are left as they were
+ *   max_tokens   rows of K4 and V4 per (sequence, head): first + count beyond it is LC_ERR_CAPACITY, nothing enqueued
+ * Host arrays are read before the call returns (a captured launch keeps their values).
+ */
+int lc_cache4_store(const void* K, const void* V, const int64_t kv_strides[3], const int32_t* first, const int32_t* counts,
+                    int B, int H_kv, int d, void* K4, void* V4, const int64_t strides4[3], int max_tokens, void* stream);
+
+/* lc_cache4_load -- rows first[b] + i of K4 and V4 as bfloat16 into rows i of K and V.  Exact: every value of the format is a bfloat16 value. */
+int lc_cache4_load(const void* K4, const void* V4, const int64_t strides4[3], const int32_t* first, const int32_t* counts,
+                   int B, int H_kv, int d, void* K, void* V, const int64_t kv_strides[3], int max_tokens, void* stream);
+
+/*
+ * lc_sparse_decode4 -- lc_sparse_decode over a 4-bit cache: the same list, active set, outputs and workspace.  The rows enter the products as the
+ * values they stand for, sums and softmax are float32.  Entries of the list that are no chunk of the sequence hold no tokens.  A token whose
+ * logit lies more than 126 powers of two below the largest weighs nothing.
+ */
+int lc_sparse_decode4(const lc_index* idx, const void* q, const void* K4, const void* V4, const int64_t strides4[3],
+                      const int32_t* chunk_ids, const int32_t* counts, int cap, int H_q,
+                      float* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* lc_append4 -- lc_append over a 4-bit cache: k_new and v_new (bfloat16) are rounded as lc_cache4_store does it, and a closing chunk is
+ * pooled from its rows as the cache holds them. */
+int lc_append4(lc_index* idx, void* K4, void* V4, const int64_t strides4[3], const void* k_new, const void* v_new,
+               const uint8_t* close_chunk, void* stream);
+
+/*
+ * Eviction of chunks by the attention weight that they have gathered.  The caller keeps weights, float32 [B][H_kv][cfg.max_chunks], zero at first:
+ * per step  lc_weigh_chunks adds what the step's attention gave each chunk;
+ * at times  lc_evict_select picks the chunks that stay, lc_evict_rows writes the cache without the others, and lc_build_index over
+ *           that cache (with keep_bounds as its chunk_bounds) makes its index.
+ *
+ * lc_weigh_chunks -- for every listed chunk c of (b, h)
+ *   weights[b][h][c] += sum over its tokens t and the group's heads g of exp(q_g . k_t / sqrt(d) - lse_g).
+ *   chunk_ids, counts, cap   as in lc_sparse_decode, ascending; an entry that is no chunk of the sequence, or no larger than the entry before it,
+ *                            is passed over
+ *   lse        float32 [B][H_q] as lc_sparse_decode or lc_decode_step gave it for the same q; a head with -inf adds nothing
+ * The same bits every time; every chunk is added to once.  Chunks that are not listed, and the open tail, are not touched.
+ */
+int lc_weigh_chunks(const lc_index* idx, const void* q, const void* K, const int64_t k_strides[3], const int32_t* chunk_ids,
+                    const int32_t* counts, int cap, int H_q, const float* lse, float* weights, void* stream);
+/* ... over the keys of a 4-bit cache (byte strides). */
+int lc_weigh_chunks4(const lc_index* idx, const void* q, const void* K4, const int64_t strides4[3], const int32_t* chunk_ids,
+                     const int32_t* counts, int cap, int H_q, const float* lse, float* weights, void* stream);
+
+/*
+ * lc_evict_select -- the chunks to keep, per sequence (its heads share the boundaries, so a chunk goes or stays in all of them).  Pinned are the leading chunks that
+ * cover cfg.sink_tokens tokens and the closed chunks with a token among the last recent_tokens closed ones; of the others, ordered by
+ * (weight summed over the heads descending, id ascending), the longest prefix whose tokens and the pinned ones' total at most keep_tokens.  (If the
+ * pinned ones alone have more, they are what is kept.)  A sum that is not a number comes last.  The open tail always stays and is not counted.
+ *   keep_ids     int32 [B][max_chunks] out: ascending, then -1
+ *   keep_bounds  int32 [B][max_chunks + 1] out: where the kept chunks begin in the new cache; from keep_counts[b] on the end of the last
+ *   keep_counts  int32 [B] out
+ *   keep_lens    int32 [B] out or NULL: tokens of the new cache, the open tail's among them
+ *   ws           any workspace of lc_decode_workspace_bytes() (B * max_chunks * 8 bytes are used)
+ */
+int lc_evict_select(const lc_index* idx, const float* weights, int keep_tokens, int recent_tokens, int32_t* keep_ids, int32_t* keep_bounds,
+                    int32_t* keep_counts, int32_t* keep_lens, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * lc_evict_rows -- the rows of the kept chunks, one chunk behind the other, then the open tail's, from K and V to the first rows of K_to and V_to (of
+ * cfg.max_tokens rows per (sequence, head); rows behind are left as they were); with weights, weights_to[b][h][i] = weights[b][h][keep_ids[b][i]] and zeros behind.
+ * The destination must not overlap the source: many layers share one spare cache, which trades places with each layer's.
+ *   weights, weights_to   both or neither
+ */
+int lc_evict_rows(const lc_index* idx, const int32_t* keep_ids, const int32_t* keep_bounds, const int32_t* keep_counts, const void* K, const void* V,
+                  const int64_t kv_strides[3], void* K_to, void* V_to, const int64_t to_strides[3], const float* weights, float* weights_to, void* stream);
+/* ... of a 4-bit cache (byte strides). */
+int lc_evict_rows4(const lc_index* idx, const int32_t* keep_ids, const int32_t* keep_bounds, const int32_t* keep_counts, const void* K4, const void* V4,
+                   const int64_t strides4[3], void* K4_to, void* V4_to, const int64_t to_strides4[3], const float* weights, float* weights_to, void* stream);
+
 /* Sizes the two level walks are limited to (pure host function; either pointer may be NULL).
  *   exact_walk_internal_nodes   EXACT with the level walk on: internal nodes (all levels above the
  *                               chunks together) of one (sequence, head); the walk keeps them in LDS.

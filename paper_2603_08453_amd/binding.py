@@ -17,6 +17,7 @@ import numpy as np
 LC_MAX_LEVELS = 6
 LC_MAX_GROUP = 8
 LC_HEAD_DIM = 128
+LC_CACHE4_ROW = 68
 
 LC_OK = 0
 LC_ERR_INVALID_ARG = -1
@@ -141,6 +142,24 @@ def lib() -> ctypes.CDLL:
     L.lc_chunk_tokens.argtypes = [ctypes.c_char_p, i64p, ctypes.c_int, ctypes.c_int, ctypes.c_int,
                                   i32p, ctypes.c_int, ctypes.POINTER(ctypes.c_int)]
     L.lc_chunk_tokens.restype = ctypes.c_int
+    L.lc_cache4_store.argtypes = [vp, vp, i64p, i32p, i32p, ctypes.c_int, ctypes.c_int, ctypes.c_int, vp, vp, i64p, ctypes.c_int, vp]
+    L.lc_cache4_store.restype = ctypes.c_int
+    L.lc_cache4_load.argtypes = [vp, vp, i64p, i32p, i32p, ctypes.c_int, ctypes.c_int, ctypes.c_int, vp, vp, i64p, ctypes.c_int, vp]
+    L.lc_cache4_load.restype = ctypes.c_int
+    L.lc_sparse_decode4.argtypes = L.lc_sparse_decode.argtypes
+    L.lc_sparse_decode4.restype = ctypes.c_int
+    L.lc_append4.argtypes = [vp, vp, vp, i64p, vp, vp, u8p, vp]
+    L.lc_append4.restype = ctypes.c_int
+    for name in ("lc_weigh_chunks", "lc_weigh_chunks4"):
+        f = getattr(L, name)
+        f.argtypes = [vp, vp, vp, i64p, vp, vp, ctypes.c_int, ctypes.c_int, vp, vp, vp]
+        f.restype = ctypes.c_int
+    L.lc_evict_select.argtypes = [vp, vp, ctypes.c_int, ctypes.c_int, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    L.lc_evict_select.restype = ctypes.c_int
+    for name in ("lc_evict_rows", "lc_evict_rows4"):
+        f = getattr(L, name)
+        f.argtypes = [vp, vp, vp, vp, vp, vp, i64p, vp, vp, i64p, vp, vp, vp]
+        f.restype = ctypes.c_int
     _lib = L
     return L
 
@@ -435,6 +454,82 @@ def lc_append(idx: Index, K, V, k_new, v_new, close_chunk: Optional[Sequence[int
     rc = lib().lc_append(idx.handle, _ptr(K), _ptr(V), _strides3(K), _ptr(k_new), _ptr(v_new), cc,
                          _ptr(ws), ws.numel() * ws.element_size(), _stream(stream))
     _check(rc, "lc_append")
+
+
+# ------------------------------------------------------------------ a cache in 4 bits
+
+def _strides4(t) -> "ctypes.Array":
+    assert t.dim() == 4 and t.shape[3] == LC_CACHE4_ROW and t.stride(3) == 1 and t.element_size() == 1, \
+        "4-bit cache must be uint8 [B][H_kv][tokens][68] with a row's bytes contiguous"
+    return (ctypes.c_int64 * 3)(t.stride(0), t.stride(1), t.stride(2))
+
+
+def _move4(call, where, K, V, K4, V4, first, counts, stream, store):
+    B, H_kv, rows, d = K.shape
+    assert K.shape == V.shape and K.stride() == V.stride() and K4.shape == V4.shape and K4.stride() == V4.stride()
+    assert K4.shape[:2] == K.shape[:2] and K.element_size() == 2
+    counts = [rows] * B if counts is None else [int(n) for n in counts]
+    assert len(counts) == B and max(counts, default=0) <= rows and (first is None or len(first) == B)
+    wide, narrow = (_ptr(K), _ptr(V), _strides3(K)), (_ptr(K4), _ptr(V4), _strides4(K4))
+    range_ = (None if first is None else _i32(first), _i32(counts), B, H_kv, d)
+    a, b = (wide, narrow) if store else (narrow, wide)
+    _check(call(*a, *range_, *b, K4.shape[2], _stream(stream)), where)
+
+
+def lc_cache4_store(K, V, K4, V4, first=None, counts=None, stream=None) -> None:
+    """Rows [0, counts[b]) of K and V (bf16 [B][H_kv][rows][d]) into rows first[b] + i of K4 and V4 (uint8 [B][H_kv][tokens][68])."""
+    _move4(lib().lc_cache4_store, "lc_cache4_store", K, V, K4, V4, first, counts, stream, True)
+
+
+def lc_cache4_load(K4, V4, K, V, first=None, counts=None, stream=None) -> None:
+    """Rows first[b] + i, i < counts[b], of K4 and V4 as bf16 into rows i of K and V (exact)."""
+    _move4(lib().lc_cache4_load, "lc_cache4_load", K, V, K4, V4, first, counts, stream, False)
+
+
+def lc_sparse_decode4(idx: Index, q, K4, V4, chunk_ids, counts, out, ws, lse=None, stream=None) -> None:
+    """lc_sparse_decode over a 4-bit cache (uint8 [B][H_kv][tokens][68])."""
+    assert K4.stride() == V4.stride()
+    _check(lib().lc_sparse_decode4(idx.handle, _ptr(q), _ptr(K4), _ptr(V4), _strides4(K4), _ptr(chunk_ids), _ptr(counts),
+                                   chunk_ids.shape[2], q.shape[1], _ptr(out), _ptr(lse), _ptr(ws), ws.numel() * ws.element_size(),
+                                   _stream(stream)), "lc_sparse_decode4")
+
+
+def lc_append4(idx: Index, K4, V4, k_new, v_new, close_chunk: Optional[Sequence[int]] = None, stream=None) -> None:
+    """lc_append over a 4-bit cache."""
+    cc = None
+    if close_chunk is not None:
+        cc = (ctypes.c_uint8 * len(close_chunk))(*[1 if c else 0 for c in close_chunk])
+    assert K4.stride() == V4.stride()
+    _check(lib().lc_append4(idx.handle, _ptr(K4), _ptr(V4), _strides4(K4), _ptr(k_new), _ptr(v_new), cc, _stream(stream)), "lc_append4")
+
+
+# ------------------------------------------------------------------ eviction by accumulated attention weight
+
+def lc_weigh_chunks(idx: Index, q, K, chunk_ids, counts, lse, weights, stream=None) -> None:
+    """Adds each listed chunk's attention weight to weights (float32 [B][H_kv][max_chunks]); lse float32 [B][H_q] as lc_sparse_decode gives it."""
+    _check(lib().lc_weigh_chunks(idx.handle, _ptr(q), _ptr(K), _strides3(K), _ptr(chunk_ids), _ptr(counts), chunk_ids.shape[2], q.shape[1],
+                                 _ptr(lse), _ptr(weights), _stream(stream)), "lc_weigh_chunks")
+
+
+def lc_weigh_chunks4(idx: Index, q, K4, chunk_ids, counts, lse, weights, stream=None) -> None:
+    """lc_weigh_chunks over a 4-bit cache."""
+    _check(lib().lc_weigh_chunks4(idx.handle, _ptr(q), _ptr(K4), _strides4(K4), _ptr(chunk_ids), _ptr(counts), chunk_ids.shape[2], q.shape[1],
+                                  _ptr(lse), _ptr(weights), _stream(stream)), "lc_weigh_chunks4")
+
+
+def lc_evict_select(idx: Index, weights, keep_tokens: int, recent_tokens: int, keep_ids, keep_bounds, keep_counts, ws, keep_lens=None,
+                    stream=None) -> None:
+    """keep_ids int32 [B][max_chunks], keep_bounds int32 [B][max_chunks + 1], keep_counts int32 [B], keep_lens int32 [B] or None."""
+    _check(lib().lc_evict_select(idx.handle, _ptr(weights), int(keep_tokens), int(recent_tokens), _ptr(keep_ids), _ptr(keep_bounds),
+                                 _ptr(keep_counts), _ptr(keep_lens), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)), "lc_evict_select")
+
+
+def lc_evict_rows(idx: Index, keep_ids, keep_bounds, keep_counts, K, V, K_to, V_to, weights=None, weights_to=None, stream=None) -> None:
+    """The kept chunks' rows and the open tail's from K and V to the front of K_to and V_to; bf16 caches, or 4-bit ones (uint8)."""
+    assert K.stride() == V.stride() and K_to.stride() == V_to.stride() and K.element_size() == K_to.element_size()
+    call, strides = (lib().lc_evict_rows4, _strides4) if K.element_size() == 1 else (lib().lc_evict_rows, _strides3)
+    _check(call(idx.handle, _ptr(keep_ids), _ptr(keep_bounds), _ptr(keep_counts), _ptr(K), _ptr(V), strides(K), _ptr(K_to), _ptr(V_to),
+                strides(K_to), _ptr(weights), _ptr(weights_to), _stream(stream)), "lc_evict_rows")
 
 
 _new_bytes = ctypes.pythonapi.PyBytes_FromStringAndSize

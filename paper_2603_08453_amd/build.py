@@ -15,7 +15,7 @@ LIB = os.path.join(HERE, "liblychee.so")
 # CPython modules, host code only: source -> module, and whether it uses torch's C++ objects
 HOST_MODULES = [("lc_pyhost.cpp", os.path.join(HERE, "_lychee_host.so"), False),
                 ("lc_pytorch.cpp", os.path.join(HERE, "_lychee_torch.so"), True)]
-SOURCES = ["lc_api.hip", "lc_retrieve.hip", "lc_decode.hip", "lc_build.hip", "lc_blob.hip", "lc_chunker.hip", "lc_bench.hip"]
+SOURCES = ["lc_api.hip", "lc_retrieve.hip", "lc_decode.hip", "lc_cache4.hip", "lc_evict.hip", "lc_build.hip", "lc_blob.hip", "lc_chunker.hip", "lc_bench.hip"]
 
 
 def hipcc() -> str:

@@ -12,6 +12,7 @@
 //
 // Every reduction runs in a fixed order, so results are reproducible run to run.
 #include "lc_device.h"
+#include "lc_cache4.h"
 #include "lc_internal.h"
 #include "lc_rounds_planes.h"
 #include "lc_select.h"
@@ -36,8 +37,9 @@ __device__ __forceinline__ float lc_pad_radius(float r) { return r > 0.f ? r * (
 // sh: LC_BG * 128 + LC_BG floats.
 // ---------------------------------------------------------------------------------
 #define LC_POOL_KEEP 8            // rows per 16-lane group that stay in registers between the two passes (chunks up to 128 tokens are read once)
-__device__ __forceinline__ void lc_pool_rows(const uint16_t* __restrict__ Kbh, long long ks_tok, int lo, int hi,
-                                             int geometry, bool round_bf16, float* sh, float (&mu)[8], float* radius) {
+// row(r): columns [8 sub, 8 sub + 8) of key r as bfloat16 values
+template <typename Row>
+__device__ __forceinline__ void lc_pool_rows(Row row, int lo, int hi, int geometry, bool round_bf16, float* sh, float (&mu)[8], float* radius) {
     const int tid = threadIdx.x, sub = tid & 15, grp = tid >> 4;
     float sum[8];
 #pragma unroll
@@ -47,7 +49,7 @@ __device__ __forceinline__ void lc_pool_rows(const uint16_t* __restrict__ Kbh, l
     for (int k = 0; k < LC_POOL_KEEP; ++k) {
         const int r = lo + grp + k * LC_BG;
         keep[k] = make_uint4(0u, 0u, 0u, 0u);
-        if (r < hi) keep[k] = *reinterpret_cast<const uint4*>(Kbh + (long long)r * ks_tok + 8 * sub);
+        if (r < hi) keep[k] = row(r);
     }
 #pragma unroll
     for (int k = 0; k < LC_POOL_KEEP; ++k) {          // (rows past the chunk hold zeros: they add nothing)
@@ -57,7 +59,7 @@ __device__ __forceinline__ void lc_pool_rows(const uint16_t* __restrict__ Kbh, l
         for (int i = 0; i < 8; ++i) sum[i] += f[i];
     }
     for (int r = lo + grp + LC_POOL_KEEP * LC_BG; r < hi; r += LC_BG) {
-        const uint4 v = *reinterpret_cast<const uint4*>(Kbh + (long long)r * ks_tok + 8 * sub);
+        const uint4 v = row(r);
         float f[8];
         lc_unpack8(v, f);
 #pragma unroll
@@ -113,7 +115,7 @@ __device__ __forceinline__ void lc_pool_rows(const uint16_t* __restrict__ Kbh, l
     for (int k = 0; k < LC_POOL_KEEP; ++k)
         if (lo + grp + k * LC_BG < hi) reach(keep[k]);
     for (int r = lo + grp + LC_POOL_KEEP * LC_BG; r < hi; r += LC_BG)
-        reach(*reinterpret_cast<const uint4*>(Kbh + (long long)r * ks_tok + 8 * sub));
+        reach(row(r));
     __syncthreads();
     if (sub == 0) sh[grp] = far2;
     __syncthreads();
@@ -121,6 +123,14 @@ __device__ __forceinline__ void lc_pool_rows(const uint16_t* __restrict__ Kbh, l
     for (int g = 0; g < LC_BG; ++g) mx = fmaxf(mx, sh[g]);
     *radius = lc_pad_radius(sqrtf(mx));
     __syncthreads();
+}
+
+// ... of a bfloat16 cache
+__device__ __forceinline__ void lc_pool_rows(const uint16_t* __restrict__ Kbh, long long ks_tok, int lo, int hi,
+                                             int geometry, bool round_bf16, float* sh, float (&mu)[8], float* radius) {
+    const int sub = threadIdx.x & 15;
+    lc_pool_rows([&](int r) __attribute__((always_inline)) { return *reinterpret_cast<const uint4*>(Kbh + (long long)r * ks_tok + 8 * sub); },
+                 lo, hi, geometry, round_bf16, sh, mu, radius);
 }
 
 // unit direction of the 8-column fragments (zero vector -> e_0)
@@ -2990,9 +3000,13 @@ int lc_launch_drift(const lc_index* idx, int level, float* out, hipStream_t stre
 // ---------------------------------------------------------------------------------
 struct LcCloseBits { uint32_t w[32]; };       // one bit per sequence (B <= 1024)
 
+// Cell: uint16_t, a bfloat16 cache with strides in values; uint8_t, a cache in 4 bits with strides in bytes.  There a chunk is pooled from its rows as they are
+// stored, the values that the attention reads.
+template <typename Cell>
 __global__ void __launch_bounds__(LC_BT)
-lc_append_kernel(LcDev ix, uint16_t* K, uint16_t* V, long long ks_seq, long long ks_head, long long ks_tok,
+lc_append_kernel(LcDev ix, Cell* K, Cell* V, long long ks_seq, long long ks_head, long long ks_tok,
                  const uint16_t* k_new, const uint16_t* v_new, LcCloseBits close, int geometry, int max_tokens) {
+    constexpr bool IN4 = sizeof(Cell) == 1;
     lc_fetch_args<sizeof(LcDev) + 64 + sizeof(LcCloseBits)>();
     __shared__ float sh[LC_BG * LC_D + LC_BG];
     __shared__ float best_sim[LC_BG];
@@ -3011,10 +3025,18 @@ lc_append_kernel(LcDev ix, uint16_t* K, uint16_t* V, long long ks_seq, long long
     // The host checks the capacities against its own counts before it launches; these guards are for
     // a caller who replays the launch from a captured graph, where the host is not asked again.
     if (T >= max_tokens) return;
-    uint16_t* Kbh = K + b * ks_seq + h * ks_head;
-    uint16_t* Vbh = V + b * ks_seq + h * ks_head;
-    if (tid < 32)
-        *reinterpret_cast<uint4*>((tid < 16 ? Kbh : Vbh) + (long long)T * ks_tok + 8 * sub) = row;
+    Cell* Kbh = K + b * ks_seq + h * ks_head;
+    Cell* Vbh = V + b * ks_seq + h * ks_head;
+    if (tid < 32) {
+        if constexpr (IN4) {
+            uint8_t* const to = (tid < 16 ? Kbh : Vbh) + (long long)T * ks_tok;
+            uint32_t scale;
+            *reinterpret_cast<uint32_t*>(to + 4 * sub) = lc_pack4(row, &scale);
+            if ((sub & 3) == 0) to[64 + (sub >> 2)] = (uint8_t)scale;
+        } else {
+            *reinterpret_cast<uint4*>((tid < 16 ? Kbh : Vbh) + (long long)T * ks_tok + 8 * sub) = row;
+        }
+    }
     const bool do_close = ((close.w[b >> 5] >> (b & 31)) & 1u) && M < ix.cap[0];
     if (!do_close) {
         if (tid == 0) ix.state[bh * 4 + 0] = T + 1;
@@ -3026,7 +3048,13 @@ lc_append_kernel(LcDev ix, uint16_t* K, uint16_t* V, long long ks_seq, long long
     int* bnd = ix.bounds + (size_t)b * (ix.cap[0] + 1);
     const int lo = bnd[M], hi = T + 1;
     float mu_x[8], r_x;
-    lc_pool_rows(Kbh, ks_tok, lo, hi, geometry, ix.c0_bf16 != 0, sh, mu_x, &r_x);
+    if constexpr (IN4)
+        lc_pool_rows([&](int r) __attribute__((always_inline)) {
+            const uint8_t* const from = Kbh + (long long)r * ks_tok;
+            return lc_unpack4(*reinterpret_cast<const uint32_t*>(from + 4 * sub), lc_scale4(from[64 + (sub >> 2)]));
+        }, lo, hi, geometry, ix.c0_bf16 != 0, sh, mu_x, &r_x);
+    else
+        lc_pool_rows(Kbh, ks_tok, lo, hi, geometry, ix.c0_bf16 != 0, sh, mu_x, &r_x);
     const int n_x = hi - lo;
     int p = -1;
     if (ix.L > 1) {
@@ -3114,19 +3142,35 @@ lc_append_kernel(LcDev ix, uint16_t* K, uint16_t* V, long long ks_seq, long long
     }
 }
 
+static LcCloseBits lc_close_bits(int B, const uint8_t* close_host) {
+    LcCloseBits bits;
+    for (int i = 0; i < 32; ++i) bits.w[i] = 0u;
+    if (close_host)
+        for (int b = 0; b < B; ++b)
+            if (close_host[b]) bits.w[b >> 5] |= 1u << (b & 31);
+    return bits;
+}
+
 int lc_launch_append(const lc_index* idx, void* K, void* V, const int64_t ks[3],
                      const void* k_new, const void* v_new, const uint8_t* close_host,
                      uint32_t, hipStream_t stream) {
     const LcDev& ix = idx->dev;
-    LcCloseBits bits;
-    for (int i = 0; i < 32; ++i) bits.w[i] = 0u;
-    if (close_host)
-        for (int b = 0; b < ix.B; ++b)
-            if (close_host[b]) bits.w[b >> 5] |= 1u << (b & 31);
-    hipLaunchKernelGGL(lc_append_kernel, dim3(ix.H, ix.B), dim3(LC_BT), 0, stream, ix,
+    hipLaunchKernelGGL((lc_append_kernel<uint16_t>), dim3(ix.H, ix.B), dim3(LC_BT), 0, stream, ix,
                        static_cast<uint16_t*>(K), static_cast<uint16_t*>(V),
                        (long long)ks[0], (long long)ks[1], (long long)ks[2],
-                       static_cast<const uint16_t*>(k_new), static_cast<const uint16_t*>(v_new), bits,
+                       static_cast<const uint16_t*>(k_new), static_cast<const uint16_t*>(v_new), lc_close_bits(ix.B, close_host),
+                       idx->cfg.geometry, idx->cfg.max_tokens);
+    LC_HIP_CHECK(hipGetLastError());
+    return LC_OK;
+}
+
+int lc_launch_append4(const lc_index* idx, void* K4, void* V4, const int64_t s4[3],
+                      const void* k_new, const void* v_new, const uint8_t* close_host, hipStream_t stream) {
+    const LcDev& ix = idx->dev;
+    hipLaunchKernelGGL((lc_append_kernel<uint8_t>), dim3(ix.H, ix.B), dim3(LC_BT), 0, stream, ix,
+                       static_cast<uint8_t*>(K4), static_cast<uint8_t*>(V4),
+                       (long long)s4[0], (long long)s4[1], (long long)s4[2],
+                       static_cast<const uint16_t*>(k_new), static_cast<const uint16_t*>(v_new), lc_close_bits(ix.B, close_host),
                        idx->cfg.geometry, idx->cfg.max_tokens);
     LC_HIP_CHECK(hipGetLastError());
     return LC_OK;

@@ -1,0 +1,623 @@
+// A cache of keys and values in 4 bits: rows stored and loaded (lc_cache4_store, lc_cache4_load), and the sparse attention
+// of one decode step over it (lc_sparse_decode4).  The row format is lc_cache4.h's.
+//
+// Attention.  With x_t = q.k_t / sqrt(d) over the tokens of the listed chunks and of the open tail,
+//   out = sum_t e^(x_t - m) v_t / sum_t e^(x_t - m),   lse = m + ln sum_t e^(x_t - m),
+// in one pass over the rows: each wavefront keeps a reference m of its own (a whole number of powers of two, not below its largest logit so far), the
+// parts meet at the end.  Grid (split, KV head, sequence), 256 threads; a wavefront takes 32 tokens at a time.
+//   Q.K^T: the 16 tokens of half a step are the rows of a 16x16x32 bf16 product's A operand, lane (kg, n) holding the 32 columns [32 kg, ...) of
+//   row n -- one 16-byte load, whose scale is one byte -- as four operands of eight; the query block is the B operand.  The products leave lane
+//   (kg, n) the logits of tokens 4 kg .. 4 kg + 3 for the head of column n.
+//   P.V: a lane's eight probabilities (of the two halves) are its share of the B operand, and the eight columns [8 n, 8 n + 8) of the same eight
+//   tokens -- one 4-byte load each -- are, column by column, its share of eight A operands.  No value crosses lanes.  A probability goes in as three bfloat16 terms
+//   that add up to its float32 value; the terms of a head stand in columns of their own, whose logits are the head's once more, so that up to
+//   group size 5 one product takes all three (the matrix pipe multiplies 16 columns whatever is in them); above, the third term takes a second one.
+#include "lc_cache4.h"
+#include "lc_internal.h"
+#include "lc_select.h"
+
+#define LC_C4_THREADS 256
+#define LC_C4_ROWS 64             // rows that a workgroup stores or loads
+#define LC_C4_BATCH 64            // sequences of a launch: their row numbers are launch arguments
+#define LC_D4_THREADS 256
+#define LC_D4_WAVES (LC_D4_THREADS / 64)
+#define LC_D4_TILE 1024           // tokens of a split whose cache rows are resolved into LDS at a time
+#define LC_D4_E 8                 // listed chunks per thread and pass of the row resolution
+#define LC_D4_MAX_SPLITS 256
+#define LC_LOG2E 1.4426950408889634f
+#define LC_LN2 0.6931471805599453f
+#define LC_INLINE __attribute__((always_inline))
+
+namespace {
+
+// ---------------------------------------------------------------- rows
+struct LcRange4 { int32_t first[LC_C4_BATCH], count[LC_C4_BATCH]; };
+
+struct LcMove4Args {
+    uint16_t *K, *V;
+    uint8_t *K4, *V4;
+    long long seq, head, tok;         // strides of K and V, in values
+    long long seq4, head4, tok4;      // strides of K4 and V4, in bytes
+    LcRange4 r;
+};
+
+// Row i of the sequence's range: from row i of K or V to row first + i of K4 or V4.  16 lanes to a row, 64 rows to a workgroup; z: keys and values of
+// each sequence in turn.
+__global__ void __launch_bounds__(LC_C4_THREADS)
+lc_store4_kernel(const LcMove4Args a) {
+    const int b = blockIdx.z >> 1, h = blockIdx.y, sub = threadIdx.x & 15, grp = threadIdx.x >> 4;
+    const int n = a.r.count[b];
+    const int r0 = blockIdx.x * LC_C4_ROWS + grp;
+    if (blockIdx.x * LC_C4_ROWS >= n) return;
+    const uint16_t* src = ((blockIdx.z & 1) ? a.V : a.K) + b * a.seq + h * a.head + 8 * sub;
+    uint8_t* dst = ((blockIdx.z & 1) ? a.V4 : a.K4) + b * a.seq4 + h * a.head4 + (long long)a.r.first[b] * a.tok4;
+    uint4 v[LC_C4_ROWS / 16];
+#pragma unroll
+    for (int k = 0; k < LC_C4_ROWS / 16; ++k) {
+        const int r = r0 + 16 * k;
+        v[k] = make_uint4(0u, 0u, 0u, 0u);
+        if (r < n) v[k] = *reinterpret_cast<const uint4*>(src + r * a.tok);
+    }
+#pragma unroll
+    for (int k = 0; k < LC_C4_ROWS / 16; ++k) {
+        const int r = r0 + 16 * k;
+        uint32_t scale;
+        const uint32_t codes = lc_pack4(v[k], &scale);
+        if (r < n) {
+            uint8_t* row = dst + r * a.tok4;
+            *reinterpret_cast<uint32_t*>(row + 4 * sub) = codes;
+            if ((sub & 3) == 0) row[64 + (sub >> 2)] = (uint8_t)scale;
+        }
+    }
+}
+
+// Row first + i of K4 or V4 to row i of K or V.
+__global__ void __launch_bounds__(LC_C4_THREADS)
+lc_load4_kernel(const LcMove4Args a) {
+    const int b = blockIdx.z >> 1, h = blockIdx.y, sub = threadIdx.x & 15, grp = threadIdx.x >> 4;
+    const int n = a.r.count[b];
+    const int r0 = blockIdx.x * LC_C4_ROWS + grp;
+    if (blockIdx.x * LC_C4_ROWS >= n) return;
+    uint16_t* dst = ((blockIdx.z & 1) ? a.V : a.K) + b * a.seq + h * a.head + 8 * sub;
+    const uint8_t* src = ((blockIdx.z & 1) ? a.V4 : a.K4) + b * a.seq4 + h * a.head4 + (long long)a.r.first[b] * a.tok4;
+    uint32_t c[LC_C4_ROWS / 16], s[LC_C4_ROWS / 16];
+#pragma unroll
+    for (int k = 0; k < LC_C4_ROWS / 16; ++k) {
+        const int r = r0 + 16 * k;
+        c[k] = s[k] = 0u;
+        if (r < n) {
+            c[k] = *reinterpret_cast<const uint32_t*>(src + r * a.tok4 + 4 * sub);
+            s[k] = src[r * a.tok4 + 64 + (sub >> 2)];
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < LC_C4_ROWS / 16; ++k) {
+        const int r = r0 + 16 * k;
+        if (r < n) *reinterpret_cast<uint4*>(dst + r * a.tok) = lc_unpack4(c[k], lc_scale4(s[k]));
+    }
+}
+
+// ---------------------------------------------------------------- attention
+struct LcDecode4Args {
+    LcDev ix;
+    const uint16_t* q;
+    const uint8_t *K, *V;
+    long long seq, head;  // strides in bytes
+    int tok;
+    int max_tokens;       // rows of one (sequence, head) slab of K and V
+    const int32_t* ids;
+    const int32_t* counts;
+    int cap;
+    float* part_acc;      // [B][H][S][G][d]
+    float* part_ml;       // [B][H][S][G][2]
+    float* out;           // [B][H*G][d]
+    float* lse;           // [B][H*G] or null
+};
+
+template <int G>
+__global__ void __launch_bounds__(LC_D4_THREADS, 2)
+lc_decode4_kernel(const LcDecode4Args a) {
+    lc_fetch_args<sizeof(LcDecode4Args)>();
+    constexpr bool WIDE = G > 5;                 // three terms of a probability in three columns, or two in two and the third apart
+    constexpr int COLS = WIDE ? 16 : 3 * G;      // columns that hold something
+    constexpr int TERMS = WIDE ? 2 : 3;          // columns of a head
+    constexpr int STEP = 32;
+    constexpr int ROW = LC_D + 4;                // floats between the columns' sums in LDS: lanes of different columns use different banks
+    union Phases {
+        struct {
+            float acc[LC_D4_WAVES][COLS][ROW];
+            float ml[LC_D4_WAVES][G][2];
+        } comb;
+        struct {
+            float m[LC_MAX_GROUP * LC_D4_MAX_SPLITS], l[LC_MAX_GROUP * LC_D4_MAX_SPLITS];
+            float4 red[LC_D4_THREADS];
+        } merge;
+        int row[LC_D4_TILE];                     // byte offsets of the cache rows of the tile's tokens
+    };
+    __shared__ __attribute__((aligned(16))) Phases ph;
+    __shared__ int scan_sh[8];
+    __shared__ int last_sh;
+
+    const LcDev& ix = a.ix;
+    const int s = blockIdx.x, S = gridDim.x, h = blockIdx.y, b = blockIdx.z;
+    const int bh = b * ix.H + h;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, kg = lane >> 4;
+    // the head and the term of this lane's column
+    const int term = WIDE ? n >> 3 : n / G;
+    const int head = WIDE ? min(n & 7, G - 1) : n - term * G;
+
+    const __amdgpu_buffer_rsrc_t bnd_r = lc_buffer(ix.bounds + (size_t)b * (ix.cap[0] + 1), (ix.cap[0] + 1) * 4);
+    const __amdgpu_buffer_rsrc_t ids_r = lc_buffer(a.ids + (size_t)bh * a.cap, (int)(min((long long)a.cap, 1LL << 28) * 4));
+
+    // ---- the attended tokens: the listed chunks in the list's order, then the open tail.  Thread t of a pass owns entries [E t, E t + E);
+    // the first pass stays in registers.
+    constexpr int E = LC_D4_E, PASS = E * LC_D4_THREADS;
+    lc_v4i idv[E / 4];
+    auto load_ids = [&](int base) LC_INLINE {
+#pragma unroll
+        for (int e = 0; e < E / 4; ++e) idv[e] = __builtin_amdgcn_raw_buffer_load_b128(ids_r, (base + tid * E) * 4, 16 * e, 0);
+    };
+    load_ids(0);
+    uint4 qb[4];
+    {
+        const uint16_t* qh = a.q + ((size_t)b * ix.H * G + (size_t)h * G + head) * LC_D + 32 * kg;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) qb[c] = *reinterpret_cast<const uint4*>(qh + 8 * c);
+    }
+    const int T = ix.state[bh * 4 + 0], M = ix.state[bh * 4 + 1];
+    const int n_ids = max(0, min(a.counts[bh], a.cap));
+    const int tail_st = lc_buf_load_i32(bnd_r, M), tail_ln = max(0, T - tail_st);
+    // (an entry that is no chunk holds no tokens)
+    auto entries = [&](int base, int (&st)[E], int (&ln)[E]) LC_INLINE -> int {
+        int sum = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int id = idv[e / 4][e % 4];
+            const bool real = base + tid * E + e < n_ids && id >= 0 && id < M;
+            // (branch-free: a load past the resource's end gives zeros)
+            const lc_v2i x = __builtin_amdgcn_raw_buffer_load_b64(bnd_r, real ? id * 4 : 0x7ffffff0, 0, 0);
+            st[e] = x.x;
+            ln[e] = x.y;
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            ln[e] = max(0, ln[e] - st[e]);
+            sum += ln[e];
+        }
+        return sum;
+    };
+    int st0[E], ln0[E], tot0;
+    const int ex0 = lc_block_scan<LC_D4_THREADS>(entries(0, st0, ln0), scan_sh, &tot0);
+    int n_sel = tot0;
+    for (int base = PASS; base < n_ids; base += PASS) {
+        int st[E], ln[E], tot;
+        load_ids(base);
+        lc_block_scan<LC_D4_THREADS>(entries(base, st, ln), scan_sh, &tot);
+        n_sel += tot;
+    }
+    const int n_tok = n_sel + tail_ln;
+    const int S_eff = max(1, min(S, (n_tok + LC_DEC_MIN_TOKENS_PER_SPLIT - 1) / LC_DEC_MIN_TOKENS_PER_SPLIT));
+    if (s >= S_eff) return;                      // (the same n_tok in all of them: nobody waits for these)
+
+    const float scale = 0.08838834764831845f * LC_LOG2E;     // log2(e) / sqrt(128)
+    // The softmax of column n's head over the wavefront's tokens; acc[c][r]: column 8 (4 kg + r) + c of the values.
+    float m_ref = LC_NEG_INF, l_run = 0.f;
+    lc_f32x4 acc[8];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) acc[c] = lc_f32x4{0.f, 0.f, 0.f, 0.f};
+    // (the resources end with the last row the index may ever hold: past it, where tokens that are not there are read, loads give zeros)
+    const int slab_bytes = (a.max_tokens - 1) * a.tok + LC_ROW4;
+    const __amdgpu_buffer_rsrc_t Kr = lc_buffer(a.K + (size_t)b * a.seq + (size_t)h * a.head, slab_bytes);
+    const __amdgpu_buffer_rsrc_t Vr = lc_buffer(a.V + (size_t)b * a.seq + (size_t)h * a.head, slab_bytes);
+
+    struct Step {
+        lc_v4i k[2];
+        int ks[2];
+        int v[8], vs[8];
+    };
+    auto load = [&](Step& w, int i) LC_INLINE {
+        int ko[2], vo[8];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) ko[t] = ph.row[i + 16 * t + n];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const lc_v4i r = *reinterpret_cast<const lc_v4i*>(&ph.row[i + 16 * t + 4 * kg]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) vo[4 * t + j] = r[j];
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            w.k[t] = __builtin_amdgcn_raw_buffer_load_b128(Kr, ko[t] + 16 * kg, 0, 0);
+            w.ks[t] = lc_buf_load_u8(Kr, ko[t] + 64 + kg);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w.v[j] = __builtin_amdgcn_raw_buffer_load_b32(Vr, vo[j] + 4 * n, 0, 0);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w.vs[j] = lc_buf_load_u8(Vr, vo[j] + 64 + (n >> 2));
+    };
+    auto attend = [&](const Step& w, int i, int end) LC_INLINE {
+        float x[8];
+        float mx = LC_NEG_INF;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            lc_f32x4 d = {0.f, 0.f, 0.f, 0.f};
+            const float f = lc_scale4((uint32_t)w.ks[t]);
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(lc_bf16x8, lc_unpack4((uint32_t)w.k[t][c], f)),
+                                                            __builtin_bit_cast(lc_bf16x8, qb[c]), d, 0, 0, 0);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                x[4 * t + r] = i + 16 * t + 4 * kg + r < end ? d[r] : LC_NEG_INF;
+                mx = fmaxf(mx, x[4 * t + r]);
+            }
+        }
+        mx = lc_max_groups(mx) * scale;
+        // (a whole number: scaling the sums by the difference of two rounds nothing)
+        if (__ballot(mx > m_ref) != 0ull) {
+            const float m_new = mx > m_ref ? ceilf(mx) : m_ref;
+            const float by = __builtin_amdgcn_exp2f(m_ref - m_new);
+            const float f = m_ref == m_new ? 1.f : by;
+            m_ref = m_new;
+            l_run *= f;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) acc[c] *= f;
+        }
+        const float ref = m_ref == LC_NEG_INF ? 0.f : m_ref;
+        float p[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(x[j], scale, -ref));
+        l_run += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+        // the column's term of each probability: the upper eight bits of what the terms before have left
+        lc_v4i t0, t1;
+        {
+            uint32_t w0[8], w1[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float r1 = p[j] - __uint_as_float(__float_as_uint(p[j]) & 0xffff0000u);
+                const float r2 = r1 - __uint_as_float(__float_as_uint(r1) & 0xffff0000u);
+                if constexpr (WIDE) {
+                    w0[j] = __float_as_uint(term == 0 ? p[j] : r1);
+                    w1[j] = __float_as_uint(term == 0 ? r2 : 0.f);
+                } else {
+                    w0[j] = __float_as_uint(term == 0 ? p[j] : term == 1 ? r1 : term == 2 ? r2 : 0.f);
+                    w1[j] = 0u;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                t0[j] = (int)__builtin_amdgcn_perm(w0[2 * j + 1], w0[2 * j], 0x07060302u);
+                t1[j] = (int)__builtin_amdgcn_perm(w1[2 * j + 1], w1[2 * j], 0x07060302u);
+            }
+        }
+#pragma unroll
+        for (int q2 = 0; q2 < 4; ++q2) {                        // columns 2 q2 and 2 q2 + 1 of this lane's eight
+            uint32_t y[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float f = lc_scale4((uint32_t)w.vs[j]);
+                const uint32_t c = (uint32_t)w.v[j];
+                y[j] = __builtin_bit_cast(uint32_t, q2 == 0   ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, f, 0)
+                                                    : q2 == 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, f, 1)
+                                                    : q2 == 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, f, 2)
+                                                              : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, f, 3));
+            }
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                lc_v4i v;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = (int)__builtin_amdgcn_perm(y[2 * j + 1], y[2 * j], c ? 0x07060302u : 0x05040100u);
+                lc_f32x4& o = acc[2 * q2 + c];
+                if constexpr (WIDE)
+                    o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(lc_bf16x8, v), __builtin_bit_cast(lc_bf16x8, t1), o, 0, 0, 0);
+                o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(lc_bf16x8, v), __builtin_bit_cast(lc_bf16x8, t0), o, 0, 0, 0);
+            }
+        }
+    };
+
+    // ---- the split's tokens, in tiles whose rows the workgroup first writes into LDS
+    const int lo = (int)((long long)n_tok * s / S_eff), hi = (int)((long long)n_tok * (s + 1) / S_eff);
+    const int row_max = max(T - 1, 0);
+    for (int tile0 = lo; tile0 < hi; tile0 += LC_D4_TILE) {
+        const int tl = min(LC_D4_TILE, hi - tile0);
+        auto fill = [&](int o, int st, int ln) LC_INLINE {
+            const int k0 = max(o, tile0), k1 = min(o + ln, tile0 + tl);
+            for (int k = k0 + lane; k < k1; k += 64) ph.row[k - tile0] = min(st + (k - o), row_max) * a.tok;
+        };
+        // 64 lanes per chunk that overlaps the tile (its lane's values are read by number)
+        auto visit = [&](int off, const int (&st)[E], const int (&ln)[E]) LC_INLINE {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                unsigned long long mask = __ballot(ln[e] > 0 && off < tile0 + tl && tile0 < off + ln[e]);
+                while (mask != 0ull) {
+                    const int l = __ffsll((long long)mask) - 1;
+                    mask &= mask - 1ull;
+                    fill(lc_readlane(off, l), lc_readlane(st[e], l), lc_readlane(ln[e], l));
+                }
+                off += ln[e];
+            }
+        };
+        if (tile0 != lo) __syncthreads();                           // the previous tile's rows have been used
+        visit(ex0, st0, ln0);
+        int carry = tot0;
+        for (int base = PASS; base < n_ids; base += PASS) {
+            int st[E], ln[E], tot;
+            load_ids(base);
+            const int ex = lc_block_scan<LC_D4_THREADS>(entries(base, st, ln), scan_sh, &tot);
+            visit(carry + ex, st, ln);
+            carry += tot;
+        }
+        if (wave == 0 && tail_ln > 0 && n_sel < tile0 + tl && tile0 < n_sel + tail_ln) fill(n_sel, tail_st, tail_ln);
+        const int steps = (tl + STEP - 1) / STEP;
+        for (int k = tl + tid; k < steps * STEP; k += LC_D4_THREADS) ph.row[k] = slab_bytes;
+        __syncthreads();
+        // a step's rows are fetched while the one before is computed
+        Step x, y;
+        int i = wave;
+        if (i < steps) load(x, i * STEP);
+        for (; i < steps; i += 2 * LC_D4_WAVES) {
+            const int j = i + LC_D4_WAVES, k = i + 2 * LC_D4_WAVES;
+            if (j < steps) load(y, j * STEP);
+            attend(x, i * STEP, tl);
+            if (k < steps) load(x, k * STEP);
+            if (j < steps) attend(y, j * STEP, tl);
+        }
+    }
+
+    // ---- the wavefronts' sums meet in LDS
+    __syncthreads();
+    {
+        float l = lc_add_halves(l_run, l_run);
+        l = lc_add_rows(l, l);
+        if (kg == 0 && term == 0 && n < G) { ph.comb.ml[wave][head][0] = m_ref; ph.comb.ml[wave][head][1] = l; }
+        if (n < COLS) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float4* const o = reinterpret_cast<float4*>(&ph.comb.acc[wave][n][8 * (4 * kg + r)]);
+                o[0] = make_float4(acc[0][r], acc[1][r], acc[2][r], acc[3][r]);
+                o[1] = make_float4(acc[4][r], acc[5][r], acc[6][r], acc[7][r]);
+            }
+        }
+    }
+    __syncthreads();
+    auto finish = [&](int g, int c4, float4 num, float m, float den) LC_INLINE {
+        const float inv = den == 0.f ? 0.f : 1.0f / den;           // (no tokens: zeros)
+        const size_t o = (size_t)b * ix.H * G + (size_t)h * G + g;
+        *reinterpret_cast<float4*>(a.out + o * LC_D + 4 * c4) = make_float4(num.x * inv, num.y * inv, num.z * inv, num.w * inv);
+        if (a.lse && c4 == 0) {
+            int e = 0;                                              // (whole powers of two aside, the logarithm is of a number near 1)
+            const float part = den > 0.f ? frexpf(den, &e) : den;
+            a.lse[o] = den == 0.f ? LC_NEG_INF : fmaf(m + (float)e, LC_LN2, logf(part));
+        }
+    };
+    constexpr int NV = G * (LC_D / 4);                       // float4 slots of the output
+    {
+        float* pml = a.part_ml + ((size_t)bh * S + s) * G * 2;
+        const __amdgpu_buffer_rsrc_t pacc_w = lc_buffer(a.part_acc + ((size_t)bh * S + s) * G * LC_D, G * LC_D * 4);
+        for (int v = tid; v < NV; v += LC_D4_THREADS) {
+            const int g = v / (LC_D / 4), c4 = v % (LC_D / 4);
+            float m = LC_NEG_INF;
+#pragma unroll
+            for (int w = 0; w < LC_D4_WAVES; ++w) m = fmaxf(m, ph.comb.ml[w][g][0]);
+            const float ref = m == LC_NEG_INF ? 0.f : m;
+            float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+            float den = 0.f;
+#pragma unroll
+            for (int w = 0; w < LC_D4_WAVES; ++w) {
+                const float f = exp2f(ph.comb.ml[w][g][0] - ref);
+#pragma unroll
+                for (int t = TERMS - 1; t >= 0; --t) {
+                    const float4 x = *reinterpret_cast<const float4*>(&ph.comb.acc[w][WIDE ? 8 * t + g : t * G + g][4 * c4]);
+                    num.x = fmaf(x.x, f, num.x); num.y = fmaf(x.y, f, num.y);
+                    num.z = fmaf(x.z, f, num.z); num.w = fmaf(x.w, f, num.w);
+                }
+                den = fmaf(ph.comb.ml[w][g][1], f, den);
+            }
+            if (S_eff == 1) {
+                finish(g, c4, num, ref, den);
+            } else {
+                lc_store_agent4(pacc_w, v * 16, num);
+                if (c4 == 0) { lc_store_agent(&pml[2 * g], m); lc_store_agent(&pml[2 * g + 1], den); }
+            }
+        }
+    }
+    if (S_eff == 1) return;
+
+    // ---- the last split to arrive merges
+    if (!lc_arrive_last(&ix.sync[bh * 4 + 1], S_eff, &last_sh)) return;
+    const __amdgpu_buffer_rsrc_t pacc_r = lc_buffer(a.part_acc + (size_t)bh * S * G * LC_D, S_eff * G * LC_D * 4);
+    const float* pml = a.part_ml + (size_t)bh * S * G * 2;
+    constexpr int WAYS = (LC_D4_THREADS / NV) > 0 ? (LC_D4_THREADS / NV) : 1;
+    constexpr int MR = 8;                                    // partials per round and thread
+    const int v = tid % NV, wy = tid / NV;
+    const int g = v / (LC_D / 4), c4 = v % (LC_D / 4);
+    float4 x[MR];
+    auto load_round = [&](int sp0) LC_INLINE {
+#pragma unroll
+        for (int k = 0; k < MR; ++k) x[k] = lc_load_agent4(pacc_r, (((sp0 + k * WAYS) * G + g) * LC_D + 4 * c4) * 4);
+    };
+    load_round(wy);
+    for (int i = tid; i < S_eff * G; i += LC_D4_THREADS) {
+        ph.merge.m[i] = lc_load_agent(pml + 2 * i);
+        ph.merge.l[i] = lc_load_agent(pml + 2 * i + 1);
+    }
+    __syncthreads();
+    float m = LC_NEG_INF;
+    for (int sp = 0; sp < S_eff; ++sp) m = fmaxf(m, ph.merge.m[sp * G + g]);
+    const float ref = m == LC_NEG_INF ? 0.f : m;
+    float den = 0.f;
+    for (int sp = 0; sp < S_eff; ++sp) den = fmaf(ph.merge.l[sp * G + g], exp2f(ph.merge.m[sp * G + g] - ref), den);
+    float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (wy < WAYS) {
+        for (int sp0 = wy; sp0 < S_eff; sp0 += MR * WAYS) {
+            if (sp0 != wy) load_round(sp0);
+#pragma unroll
+            for (int k = 0; k < MR; ++k) {
+                const int sp = sp0 + k * WAYS;
+                if (sp < S_eff) {
+                    const float f = exp2f(ph.merge.m[sp * G + g] - ref);
+                    num.x = fmaf(x[k].x, f, num.x); num.y = fmaf(x[k].y, f, num.y);
+                    num.z = fmaf(x[k].z, f, num.z); num.w = fmaf(x[k].w, f, num.w);
+                }
+            }
+        }
+    }
+    if (WAYS > 1) {
+        if (wy > 0 && wy < WAYS) ph.merge.red[(wy - 1) * NV + v] = num;
+        __syncthreads();
+    }
+    if (wy == 0) {
+#pragma unroll
+        for (int k = 1; k < WAYS; ++k) {
+            const float4 o = ph.merge.red[(k - 1) * NV + v];
+            num.x += o.x; num.y += o.y; num.z += o.z; num.w += o.w;
+        }
+        finish(g, c4, num, ref, den);
+    }
+    if (tid == 0) ix.sync[bh * 4 + 1] = 0;
+}
+
+template <int G>
+int launch_decode4(const LcDecode4Args& a, int splits, hipStream_t stream) {
+    hipLaunchKernelGGL((lc_decode4_kernel<G>), dim3(splits, a.ix.H, a.ix.B), dim3(LC_D4_THREADS), 0, stream, a);
+    LC_HIP_CHECK(hipGetLastError());
+    return LC_OK;
+}
+
+// ---------------------------------------------------------------- arguments
+bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+int check_strides16(const int64_t s[3]) {
+    if (!s) return LC_ERR_INVALID_ARG;
+    for (int i = 0; i < 3; ++i)
+        if (s[i] < 0 || s[i] % 8 != 0) return LC_ERR_BAD_SHAPE;
+    return s[2] < LC_HEAD_DIM ? LC_ERR_BAD_SHAPE : LC_OK;
+}
+
+// Rows of all sequences of a store or load, LC_C4_BATCH sequences to a launch.
+int move_rows(bool store, const void* K, const void* V, const int64_t s[3], const int32_t* first, const int32_t* counts, int B, int H_kv, int d,
+              const void* K4, const void* V4, const int64_t s4[3], int max_tokens, hipStream_t stream) {
+    if (!K || !V || !counts || !K4 || !V4 || B < 1 || H_kv < 1 || max_tokens < 1) return LC_ERR_INVALID_ARG;
+    if (d != LC_HEAD_DIM || H_kv > 65535) return LC_ERR_BAD_SHAPE;
+    int rc = check_strides16(s);
+    if (rc == LC_OK) rc = lc_check_strides4(s4);
+    if (rc) return rc;
+    if (!aligned(K, 16) || !aligned(V, 16) || !aligned(K4, 4) || !aligned(V4, 4)) return LC_ERR_INVALID_ARG;
+    for (int b = 0; b < B; ++b) {
+        if (counts[b] < 0 || (first && first[b] < 0)) return LC_ERR_INVALID_ARG;
+        if ((long long)counts[b] + (first ? first[b] : 0) > max_tokens) return LC_ERR_CAPACITY;
+    }
+    for (int b0 = 0; b0 < B; b0 += LC_C4_BATCH) {
+        LcMove4Args a;
+        const int nb = B - b0 < LC_C4_BATCH ? B - b0 : LC_C4_BATCH;
+        a.K = static_cast<uint16_t*>(const_cast<void*>(K)) + b0 * s[0];
+        a.V = static_cast<uint16_t*>(const_cast<void*>(V)) + b0 * s[0];
+        a.K4 = static_cast<uint8_t*>(const_cast<void*>(K4)) + b0 * s4[0];
+        a.V4 = static_cast<uint8_t*>(const_cast<void*>(V4)) + b0 * s4[0];
+        a.seq = s[0]; a.head = s[1]; a.tok = s[2];
+        a.seq4 = s4[0]; a.head4 = s4[1]; a.tok4 = s4[2];
+        int most = 0;
+        for (int i = 0; i < LC_C4_BATCH; ++i) {
+            a.r.first[i] = i < nb && first ? first[b0 + i] : 0;
+            a.r.count[i] = i < nb ? counts[b0 + i] : 0;
+            if (a.r.count[i] > most) most = a.r.count[i];
+        }
+        if (most == 0) continue;
+        const dim3 grid((most + LC_C4_ROWS - 1) / LC_C4_ROWS, H_kv, 2 * nb);
+        if (store) hipLaunchKernelGGL(lc_store4_kernel, grid, dim3(LC_C4_THREADS), 0, stream, a);
+        else hipLaunchKernelGGL(lc_load4_kernel, grid, dim3(LC_C4_THREADS), 0, stream, a);
+        LC_HIP_CHECK(hipGetLastError());
+    }
+    return LC_OK;
+}
+
+}  // namespace
+
+int lc_check_strides4(const int64_t s[3]) {
+    if (!s) return LC_ERR_INVALID_ARG;
+    for (int i = 0; i < 3; ++i)
+        if (s[i] < 0 || s[i] % 4 != 0) return LC_ERR_BAD_SHAPE;
+    return s[2] < LC_ROW4 ? LC_ERR_BAD_SHAPE : LC_OK;
+}
+
+extern "C" {
+
+int lc_cache4_store(const void* K, const void* V, const int64_t kv_strides[3], const int32_t* first, const int32_t* counts, int B, int H_kv, int d,
+                    void* K4, void* V4, const int64_t strides4[3], int max_tokens, void* stream) {
+    return move_rows(true, K, V, kv_strides, first, counts, B, H_kv, d, K4, V4, strides4, max_tokens, static_cast<hipStream_t>(stream));
+}
+
+int lc_cache4_load(const void* K4, const void* V4, const int64_t strides4[3], const int32_t* first, const int32_t* counts, int B, int H_kv, int d,
+                   void* K, void* V, const int64_t kv_strides[3], int max_tokens, void* stream) {
+    return move_rows(false, K, V, kv_strides, first, counts, B, H_kv, d, K4, V4, strides4, max_tokens, static_cast<hipStream_t>(stream));
+}
+
+int lc_sparse_decode4(const lc_index* idx, const void* q, const void* K4, const void* V4, const int64_t strides4[3],
+                      const int32_t* chunk_ids, const int32_t* counts, int cap, int H_q, float* out, float* lse,
+                      void* ws, size_t ws_bytes, void* stream) {
+    if (!idx || !q) return LC_ERR_INVALID_ARG;
+    if (H_q < idx->H_kv || H_q % idx->H_kv != 0 || H_q / idx->H_kv > LC_MAX_GROUP) return LC_ERR_BAD_SHAPE;
+    if (cap < 1 || !K4 || !V4 || !chunk_ids || !counts || !out || !ws) return LC_ERR_INVALID_ARG;
+    const int rc = lc_check_strides4(strides4);
+    if (rc) return rc;
+    if (!aligned(q, 16) || !aligned(out, 16) || !aligned(K4, 4) || !aligned(V4, 4) || !aligned(ws, 256)) return LC_ERR_INVALID_ARG;
+    const int G = H_q / idx->H_kv;
+    int splits = lc_auto_splits(&idx->cfg, idx->B, idx->H_kv);
+    if (ws_bytes < lc_layout_ws(&idx->cfg, idx->B, H_q, idx->H_kv, idx->d, splits, nullptr, nullptr, false)) return LC_ERR_WORKSPACE_TOO_SMALL;
+    // the kernel addresses the rows of one (sequence, head) with 32-bit byte offsets
+    if ((long long)idx->cfg.max_tokens * strides4[2] >= (1LL << 31) - 128) return LC_ERR_BAD_SHAPE;
+    LcWs w;
+    lc_layout_ws(&idx->cfg, idx->B, H_q, idx->H_kv, idx->d, splits, ws, &w, false);
+    LcDecode4Args a;
+    a.ix = idx->dev;
+    a.q = static_cast<const uint16_t*>(q);
+    a.K = static_cast<const uint8_t*>(K4);
+    a.V = static_cast<const uint8_t*>(V4);
+    a.seq = strides4[0]; a.head = strides4[1]; a.tok = (int)strides4[2];
+    a.max_tokens = idx->cfg.max_tokens;
+    a.ids = chunk_ids;
+    a.counts = counts;
+    a.cap = cap;
+    a.part_acc = w.part_acc;
+    a.part_ml = w.part_ml;
+    a.out = out;
+    a.lse = lse;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    switch (G) {
+        case 1: return launch_decode4<1>(a, splits, st);
+        case 2: return launch_decode4<2>(a, splits, st);
+        case 3: return launch_decode4<3>(a, splits, st);
+        case 4: return launch_decode4<4>(a, splits, st);
+        case 5: return launch_decode4<5>(a, splits, st);
+        case 6: return launch_decode4<6>(a, splits, st);
+        case 7: return launch_decode4<7>(a, splits, st);
+        default: return launch_decode4<8>(a, splits, st);
+    }
+}
+
+int lc_append4(lc_index* idx, void* K4, void* V4, const int64_t strides4[3], const void* k_new, const void* v_new,
+               const uint8_t* close_chunk, void* stream) {
+    if (!idx || !K4 || !V4 || !k_new || !v_new) return LC_ERR_INVALID_ARG;
+    int rc = lc_check_strides4(strides4);
+    if (rc) return rc;
+    if (!aligned(K4, 4) || !aligned(V4, 4) || !aligned(k_new, 16) || !aligned(v_new, 16)) return LC_ERR_INVALID_ARG;
+    if (idx->B > 1024) return LC_ERR_CAPACITY;
+    for (int b = 0; b < idx->B; ++b) {
+        if (idx->T[b] + 1 > idx->cfg.max_tokens) return LC_ERR_CAPACITY;
+        if (close_chunk && close_chunk[b] && idx->M[b] + 1 > idx->cfg.max_chunks) return LC_ERR_CAPACITY;
+    }
+    rc = lc_launch_append4(idx, K4, V4, strides4, k_new, v_new, close_chunk, static_cast<hipStream_t>(stream));
+    if (rc != LC_OK) return rc;
+    for (int b = 0; b < idx->B; ++b) {
+        idx->T[b] += 1;
+        idx->tail[b] += 1;
+        if (close_chunk && close_chunk[b]) {
+            idx->tail[b] = 0;
+            idx->M[b] += 1;
+            idx->N[(size_t)b * LC_MAX_LEVELS + 0] = idx->M[b];
+        }
+    }
+    return LC_OK;
+}
+
+}  // extern "C"

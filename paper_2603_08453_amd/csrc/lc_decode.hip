@@ -27,6 +27,7 @@
 #include "lc_device.h"
 #include "lc_internal.h"
 #include "lc_select.h"
+#include "lc_wave.h"
 
 #ifndef LC_DEC_THREADS
 #define LC_DEC_THREADS 256
@@ -41,9 +42,6 @@
 #define LC_DEC_E 2                // selected ids per thread and pass of the row resolution
 #define LC_LOG2E 1.4426950408889634f
 #define LC_LN2 0.6931471805599453f
-
-typedef __bf16 lc_bf16x8 __attribute__((ext_vector_type(8)));
-typedef float lc_f32x4 __attribute__((ext_vector_type(4)));
 
 
 struct LcDecodeArgs {
@@ -93,23 +91,6 @@ __device__ __forceinline__ void lc_split3(const float (&p)[N], int (&t)[3][N / 2
 #pragma unroll
         for (int k = 0; k < N / 2; ++k) t[s][k] = (int)__builtin_amdgcn_perm(w[2 * k + 1], w[2 * k], 0x07060302u);   // the upper halves
     }
-}
-// a in the lower half of the wavefront and b in the upper half, each summed over the two halves
-__device__ __forceinline__ float lc_add_halves(float a, float b) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-// a in the even 16-lane rows and b in the odd ones, each summed over a row and its neighbour
-__device__ __forceinline__ float lc_add_rows(float a, float b) {
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-// maximum over the four 16-lane groups, in every lane
-__device__ __forceinline__ float lc_max_groups(float v) {
-    const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = fmaxf(__uint_as_float(h[0]), __uint_as_float(h[1]));
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 // 2^(x - LC_DEC_LAG) of a logit that lies x above its reference, -inf included: at most 1 where x is at most LC_DEC_LAG, so that P.V
 // overflows no sooner than the values' own sum.  (The exponent is lowered behind the exponential and not in x, which would lose its lowest

@@ -1,0 +1,536 @@
+// Eviction of chunks by the attention weight that they have gathered: the weights (lc_weigh_chunks, lc_weigh_chunks4), whom to keep
+// (lc_evict_select), the cache without the others (lc_evict_rows, lc_evict_rows4).
+#include "lc_cache4.h"
+#include "lc_internal.h"
+#include "lc_select.h"
+
+#define LC_LOG2E 1.4426950408889634f
+#define LC_INLINE __attribute__((always_inline))
+#define LC_WG_THREADS 256
+#define LC_WG_WAVES (LC_WG_THREADS / 64)
+#define LC_WG_LONG 256            // tokens from which on a chunk is shared by the workgroup's wavefronts
+
+namespace {
+
+// ---------------------------------------------------------------- weights
+// weights[chunk] += sum over its tokens t and the group's heads g of e^(q_g.k_t / sqrt(d) - lse_g), what the softmax with this log-sum-exp gives the
+// chunk.  A listed chunk belongs to one wavefront (a long one to one workgroup) and is added up in a fixed order, so the result has the same bits
+// every time.  The products are the attention's: 16 tokens are the rows of four 16x16x32 operands, the heads the columns.
+struct LcWeighArgs {
+    LcDev ix;
+    const uint16_t* q;
+    const void* K;
+    long long seq, head;  // strides of K in bytes
+    int tok;
+    int max_tokens;
+    const int32_t* ids;
+    const int32_t* counts;
+    int cap;
+    const float* lse;     // [B][H*G]
+    float* weights;       // [B][H][cap0]
+};
+
+template <int G, bool IN4>
+__global__ void __launch_bounds__(LC_WG_THREADS)
+lc_weigh_kernel(const LcWeighArgs a) {
+    lc_fetch_args<sizeof(LcWeighArgs)>();
+    __shared__ float part_sh[LC_WG_WAVES];
+    const LcDev& ix = a.ix;
+    const int h = blockIdx.y, b = blockIdx.z, bh = b * ix.H + h;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, kg = lane >> 4;
+    const int head = min(n, G - 1);
+    const int count = max(0, min(a.counts[bh], a.cap)), M = ix.state[bh * 4 + 1];
+    if ((int)blockIdx.x * LC_WG_WAVES >= count) return;
+    const int32_t* ids = a.ids + (size_t)bh * a.cap;
+    const int* bnd = ix.bounds + (size_t)b * (ix.cap[0] + 1);
+    // the query block as in the attention (bfloat16 rows: lane (kg, n) has columns 8 kg + 32 j, 4-bit rows: 32 kg + 8 j)
+    uint4 qb[4];
+    {
+        const uint16_t* qh = a.q + ((size_t)bh * G + head) * LC_D;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) qb[j] = *reinterpret_cast<const uint4*>(qh + (IN4 ? 32 * kg + 8 * j : 8 * kg + 32 * j));
+    }
+    const float scale = 0.08838834764831845f * LC_LOG2E;
+    const float lse = a.lse[(size_t)bh * G + head];
+    const float off = lse == LC_NEG_INF ? LC_NEG_INF : -lse * LC_LOG2E;      // (a head that attended to nothing adds nothing)
+    constexpr int ROW = IN4 ? LC_ROW4 : 2 * LC_D;
+    const int slab_bytes = (a.max_tokens - 1) * a.tok + ROW;
+    const __amdgpu_buffer_rsrc_t Kr = lc_buffer(static_cast<const char*>(a.K) + (size_t)b * a.seq + (size_t)h * a.head, slab_bytes);
+
+    struct Keys { lc_v4i k[IN4 ? 1 : 4]; int s; };
+    // rows r .. r + 15 (past `end`: zeros)
+    auto load = [&](Keys& w, int r, int end) LC_INLINE {
+        const int o = r + n < end ? (r + n) * a.tok + 16 * kg : slab_bytes;
+#pragma unroll
+        for (int j = 0; j < (IN4 ? 1 : 4); ++j) w.k[j] = __builtin_amdgcn_raw_buffer_load_b128(Kr, o, 64 * j, 0);
+        w.s = IN4 ? lc_buf_load_u8(Kr, o + 64 - 15 * kg) : 0;
+    };
+    auto shares = [&](const Keys& w, int r, int end) LC_INLINE -> float {
+        lc_f32x4 d = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            lc_bf16x8 k;
+            if constexpr (IN4) k = __builtin_bit_cast(lc_bf16x8, lc_unpack4((uint32_t)w.k[0][j], lc_scale4((uint32_t)w.s)));
+            else k = __builtin_bit_cast(lc_bf16x8, w.k[j]);
+            d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, __builtin_bit_cast(lc_bf16x8, qb[j]), d, 0, 0, 0);
+        }
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum += r + 4 * kg + i < end ? exp2f(fmaf(d[i], scale, off)) : 0.f;
+        return sum;
+    };
+    // this wavefront's part of a chunk: 16 rows of every `step`
+    auto chunk = [&](int lo, int hi, int r0, int step) LC_INLINE -> float {
+        float sum = 0.f;
+        Keys x, y;
+        load(x, r0, hi);
+        for (int r = r0; r < hi; r += 2 * step) {
+            load(y, r + step, hi);
+            sum += shares(x, r, hi);
+            load(x, r + 2 * step, hi);
+            sum += shares(y, r + step, hi);
+        }
+        return lc_sum64(n < G ? sum : 0.f);
+    };
+    for (int e0 = blockIdx.x * LC_WG_WAVES; e0 < count; e0 += gridDim.x * LC_WG_WAVES) {
+        // (an entry that is no chunk, or no larger than the one before it, is passed over)
+        auto entry = [&](int e, int* lo, int* hi) LC_INLINE -> int {
+            const int id = ids[e], before = e > 0 ? ids[e - 1] : -1;
+            const bool real = id >= 0 && id < M && id > before;
+            *lo = real ? bnd[id] : 0;
+            *hi = real ? min(bnd[id + 1], a.max_tokens) : 0;
+            return id;
+        };
+        int lo = 0, hi = 0, id = 0;
+        if (e0 + wave < count) id = entry(e0 + wave, &lo, &hi);
+        if (hi > lo && hi - lo < LC_WG_LONG) {
+            const float sum = chunk(lo, hi, lo, 16);
+            if (lane == 0) a.weights[(size_t)bh * ix.cap[0] + id] += sum;
+        }
+        for (int w = 0; w < LC_WG_WAVES && e0 + w < count; ++w) {
+            id = entry(e0 + w, &lo, &hi);
+            if (hi - lo < LC_WG_LONG) continue;                  // (the same for the workgroup)
+            const float sum = chunk(lo, hi, lo + 16 * wave, 16 * LC_WG_WAVES);
+            if (lane == 0) part_sh[wave] = sum;
+            __syncthreads();
+            if (tid == 0) a.weights[(size_t)bh * ix.cap[0] + id] += (part_sh[0] + part_sh[1]) + (part_sh[2] + part_sh[3]);
+            __syncthreads();
+        }
+    }
+}
+
+template <bool IN4>
+int launch_weigh(const LcWeighArgs& a, int G, hipStream_t stream) {
+    // a chunk to a wavefront while there are chunks for some thousand of them
+    const int B = a.ix.B, H = a.ix.H;
+    const int parts_all = (a.cap + LC_WG_WAVES - 1) / LC_WG_WAVES;
+    const int fit = (16 * LC_COMPUTE_UNITS + B * H - 1) / (B * H);
+    const dim3 grid(parts_all < fit ? parts_all : fit, H, B);
+    switch (G) {
+        case 1: hipLaunchKernelGGL((lc_weigh_kernel<1, IN4>), grid, dim3(LC_WG_THREADS), 0, stream, a); break;
+        case 2: hipLaunchKernelGGL((lc_weigh_kernel<2, IN4>), grid, dim3(LC_WG_THREADS), 0, stream, a); break;
+        case 3: hipLaunchKernelGGL((lc_weigh_kernel<3, IN4>), grid, dim3(LC_WG_THREADS), 0, stream, a); break;
+        case 4: hipLaunchKernelGGL((lc_weigh_kernel<4, IN4>), grid, dim3(LC_WG_THREADS), 0, stream, a); break;
+        case 5: hipLaunchKernelGGL((lc_weigh_kernel<5, IN4>), grid, dim3(LC_WG_THREADS), 0, stream, a); break;
+        case 6: hipLaunchKernelGGL((lc_weigh_kernel<6, IN4>), grid, dim3(LC_WG_THREADS), 0, stream, a); break;
+        case 7: hipLaunchKernelGGL((lc_weigh_kernel<7, IN4>), grid, dim3(LC_WG_THREADS), 0, stream, a); break;
+        default: hipLaunchKernelGGL((lc_weigh_kernel<8, IN4>), grid, dim3(LC_WG_THREADS), 0, stream, a); break;
+    }
+    LC_HIP_CHECK(hipGetLastError());
+    return LC_OK;
+}
+
+// ---------------------------------------------------------------- whom to keep
+#define LC_EV_THREADS 1024
+#define LC_EV_DIGIT 11
+#define LC_EV_BINS (1 << LC_EV_DIGIT)
+#define LC_EV_FEW 256             // chunks among which the cut is found by comparing each with each
+
+// Order-preserving map of a double: larger weight, larger key; what is not a number comes last (key 0).
+__device__ __forceinline__ unsigned long long lc_weight_key(double w) {
+    if (!(w == w)) return 0ull;
+    const unsigned long long u = (unsigned long long)__double_as_longlong(w + 0.0);
+    return (u >> 63) ? ~u : (u | (1ull << 63));
+}
+
+// A sequence's chunks with their weight summed over the heads (in 64 bits, so that the order does not hang on the sum's), as keys.
+__global__ void __launch_bounds__(256)
+lc_evict_keys_kernel(LcDev ix, const float* weights, unsigned long long* keys) {
+    const int b = blockIdx.y, M = min(ix.state[b * ix.H * 4 + 1], ix.cap[0]);
+    for (int j = blockIdx.x * 256 + threadIdx.x; j < M; j += gridDim.x * 256) {
+        const float* w = weights + (size_t)b * ix.H * ix.cap[0] + j;
+        double sum = 0.0;
+        for (int h = 0; h < ix.H; ++h) sum += (double)w[(size_t)h * ix.cap[0]];
+        keys[(size_t)b * ix.cap[0] + j] = lc_weight_key(sum);
+    }
+}
+
+struct LcEvictArgs {
+    LcDev ix;
+    const unsigned long long* keys;
+    int32_t *ids, *bounds, *counts, *lens;
+    int keep, recent, sink;
+};
+
+__device__ __forceinline__ unsigned long long lc_shfl_xor64(unsigned long long v, int m) {
+    const uint32_t lo = __shfl_xor((uint32_t)v, m), hi = __shfl_xor((uint32_t)(v >> 32), m);
+    return ((unsigned long long)hi << 32) | lo;
+}
+
+// One workgroup per sequence: the pinned chunks, and of the others the longest prefix by (key descending, id ascending) that fits.  The cut
+// is found digit by digit from the first bit in which keys differ: tokens per digit, then the digit at which their sum from above no longer fits.
+__global__ void __launch_bounds__(LC_EV_THREADS)
+lc_evict_select_kernel(const LcEvictArgs a) {
+    lc_fetch_args<sizeof(LcEvictArgs)>();
+    constexpr int NT = LC_EV_THREADS, NW = NT / 64;
+    __shared__ int tok_sh[LC_EV_BINS], cnt_sh[LC_EV_BINS];
+    __shared__ unsigned long long key_sh[LC_EV_FEW], red_sh[2 * NW];
+    __shared__ int id_sh[LC_EV_FEW], len_sh[LC_EV_FEW], keep_sh[LC_EV_FEW];
+    __shared__ int scan_sh[2 * NW], found_sh[4], few_sh;
+    const LcDev& ix = a.ix;
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int T = ix.state[b * ix.H * 4 + 0], M = min(ix.state[b * ix.H * 4 + 1], ix.cap[0]);
+    const int* bnd = ix.bounds + (size_t)b * (ix.cap[0] + 1);
+    const unsigned long long* keys = a.keys + (size_t)b * ix.cap[0];
+    const int last = bnd[M];
+    auto pinned = [&](int begin, int end) { return begin < a.sink || end > last - a.recent; };
+
+    // tokens of the pinned chunks and of the others; the smallest and the largest key of those
+    int pin = 0;
+    unsigned long long lo = ~0ull, hi = 0ull;
+    for (int j = tid; j < M; j += NT) {
+        const int begin = bnd[j], end = bnd[j + 1];
+        if (pinned(begin, end)) {
+            pin += end - begin;
+        } else {
+            const unsigned long long k = keys[j];
+            lo = min(lo, k);
+            hi = max(hi, k);
+        }
+    }
+    int pin_all;
+    lc_block_scan<NT>(pin, scan_sh, &pin_all);
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        lo = min(lo, lc_shfl_xor64(lo, m));
+        hi = max(hi, lc_shfl_xor64(hi, m));
+    }
+    if (lane == 0) { red_sh[wave] = lo; red_sh[NW + wave] = hi; }
+    __syncthreads();
+    for (int w = 0; w < NW; ++w) {
+        lo = min(lo, red_sh[w]);
+        hi = max(hi, red_sh[NW + w]);
+    }
+    int left = max(0, a.keep - pin_all);                     // tokens for the others
+
+    // Keys above `above` are kept, those below are not; of those with the bits of `cut` above `shift` the first `left` tokens' worth.
+    unsigned long long cut = 0ull;
+    int shift = 64;                                          // (64: every key)
+    bool all = last - pin_all <= left;
+    int few = -1;                                            // chunks around the cut in the lists, if there are not many
+    if (!all && lo < hi) shift = 64 - __clzll((long long)(lo ^ hi));
+    if (!all) cut = shift == 64 ? 0ull : lo >> shift;
+    auto inside = [&](unsigned long long k) { return shift == 64 || (k >> shift) == cut; };
+    if (!all && lo == hi) { shift = 0; cut = lo; }
+    while (!all && shift > 0 && few < 0) {
+        const int next = max(0, shift - LC_EV_DIGIT), digits = 1 << (shift - next);
+        for (int i = tid; i < LC_EV_BINS; i += NT) tok_sh[i] = cnt_sh[i] = 0;
+        __syncthreads();
+        for (int j = tid; j < M; j += NT) {
+            const int begin = bnd[j], end = bnd[j + 1];
+            const unsigned long long k = keys[j];
+            if (!pinned(begin, end) && inside(k)) {
+                const int d = (int)((k >> next) & (unsigned long long)(digits - 1));
+                atomicAdd(&tok_sh[d], end - begin);
+                atomicAdd(&cnt_sh[d], 1);
+            }
+        }
+        __syncthreads();
+        // from the largest digit down: thread t has digits (BINS - 1 - 2 t) and the one below
+        const int d1 = LC_EV_BINS - 1 - 2 * tid, t1 = tok_sh[d1], t0 = tok_sh[d1 - 1];
+        int total;
+        const int before = lc_block_scan<NT>(t1 + t0, scan_sh, &total);
+        if (before <= left && before + t1 > left) { found_sh[0] = d1; found_sh[1] = before; found_sh[2] = cnt_sh[d1]; }
+        else if (before + t1 <= left && before + t1 + t0 > left) { found_sh[0] = d1 - 1; found_sh[1] = before + t1; found_sh[2] = cnt_sh[d1 - 1]; }
+        __syncthreads();
+        cut = (shift == 64 ? 0ull : cut << (shift - next)) | (unsigned long long)found_sh[0];
+        left -= found_sh[1];
+        shift = next;
+        if (found_sh[2] <= LC_EV_FEW) few = found_sh[2];
+        __syncthreads();
+    }
+    if (few >= 0) {
+        // the chunks at the cut, compared with each other
+        if (tid == 0) few_sh = 0;
+        __syncthreads();
+        for (int j = tid; j < M; j += NT) {
+            const int begin = bnd[j], end = bnd[j + 1];
+            const unsigned long long k = keys[j];
+            if (!pinned(begin, end) && inside(k)) {
+                const int i = atomicAdd(&few_sh, 1);
+                key_sh[i] = k;
+                id_sh[i] = j;
+                len_sh[i] = end - begin;
+            }
+        }
+        __syncthreads();
+        if (tid < few) {
+            const unsigned long long k = key_sh[tid];
+            const int id = id_sh[tid];
+            int sum = len_sh[tid];
+            for (int i = 0; i < few; ++i)
+                if (key_sh[i] > k || (key_sh[i] == k && id_sh[i] < id)) sum += len_sh[i];
+            keep_sh[tid] = sum <= left;
+        }
+        __syncthreads();
+    }
+
+    // ids, boundaries, the rest of both lists
+    int32_t* ids = a.ids + (size_t)b * ix.cap[0];
+    int32_t* bounds = a.bounds + (size_t)b * (ix.cap[0] + 1);
+    int n_keep = 0, n_tok = 0, tied = 0;                     // so far; tokens at the cut, where all keys there are equal
+    for (int j0 = 0; j0 < M; j0 += NT) {
+        const int j = j0 + tid;
+        bool keep = false, tie = false;
+        int len = 0;
+        if (j < M) {
+            const int begin = bnd[j], end = bnd[j + 1];
+            len = end - begin;
+            keep = all || pinned(begin, end);
+            if (!keep) {
+                const unsigned long long k = keys[j];
+                if (!inside(k)) {
+                    keep = (k >> shift) > cut;
+                } else if (few >= 0) {
+                    for (int i = 0; i < few; ++i)
+                        if (id_sh[i] == j) keep = keep_sh[i] != 0;
+                } else {
+                    tie = true;
+                }
+            }
+        }
+        if (few < 0 && !all) {
+            int total;
+            const int before = lc_block_scan<NT>(tie ? len : 0, scan_sh, &total);
+            if (tie) keep = tied + before + len <= left;
+            tied = min(tied + total, 1 << 30);
+        }
+        int at, tok, n, t;
+        lc_block_scan2<NT>(keep ? 1 : 0, keep ? len : 0, scan_sh, &at, &tok, &n, &t);
+        if (keep) {
+            ids[n_keep + at] = j;
+            bounds[n_keep + at] = n_tok + tok;
+        }
+        n_keep += n;
+        n_tok += t;
+    }
+    for (int i = n_keep + tid; i < ix.cap[0]; i += NT) {
+        ids[i] = -1;
+        bounds[i] = n_tok;
+    }
+    if (tid == 0) {
+        bounds[ix.cap[0]] = n_tok;
+        a.counts[b] = n_keep;
+        if (a.lens) a.lens[b] = n_tok + max(0, T - last);
+    }
+}
+
+// ---------------------------------------------------------------- the rows that stay
+#define LC_ER_THREADS 256
+#define LC_ER_ROWS 64             // new rows of a workgroup
+
+struct LcEvictRowsArgs {
+    LcDev ix;
+    const int32_t *ids, *bounds, *counts;
+    const char *K, *V;
+    char *K_to, *V_to;
+    long long seq, head, tok, seq_to, head_to, tok_to;    // strides in bytes
+    const float* weights;
+    float* weights_to;
+    int max_tokens;
+    int row_tiles;        // workgroups that move rows; those behind move weights
+};
+
+// New rows [64 x, 64 x + 64) of a (sequence, head), keys and values: the rows of the kept chunks one behind the other, then the open tail's.
+template <int BYTES>      // of a row
+__global__ void __launch_bounds__(LC_ER_THREADS)
+lc_evict_rows_kernel(const LcEvictRowsArgs a) {
+    lc_fetch_args<sizeof(LcEvictRowsArgs)>();
+    __shared__ int bound_sh[LC_ER_ROWS + 1];
+    __shared__ int row_sh[LC_ER_ROWS];
+    const LcDev& ix = a.ix;
+    const int h = blockIdx.y, b = blockIdx.z, bh = b * ix.H + h, tid = threadIdx.x, lane = tid & 63;
+    const int cap = ix.cap[0];
+    const int32_t* ids = a.ids + (size_t)b * cap;
+    const int32_t* kept = a.bounds + (size_t)b * (cap + 1);
+    const int T = min(ix.state[bh * 4 + 0], a.max_tokens), M = min(ix.state[bh * 4 + 1], cap);
+    const int* bnd = ix.bounds + (size_t)b * (cap + 1);
+    const int n = max(0, min(a.counts[b], M));
+    if ((int)blockIdx.x >= a.row_tiles) {
+        const int i = ((int)blockIdx.x - a.row_tiles) * LC_ER_THREADS + tid;
+        if (i >= cap) return;
+        const int id = i < n ? ids[i] : -1;
+        a.weights_to[(size_t)bh * cap + i] = id >= 0 && id < M ? a.weights[(size_t)bh * cap + id] : 0.f;
+        return;
+    }
+    const int last = bnd[M], n_kept = max(0, min(kept[n], T)), rows = min(n_kept + max(0, T - last), a.max_tokens);
+    // (the grid is laid out for the host's count of tokens; a captured graph may find more)
+    for (int r0 = blockIdx.x * LC_ER_ROWS; r0 < rows; r0 += a.row_tiles * LC_ER_ROWS) {
+        // the last kept chunk that begins at or before r0: 64 boundaries at a time, each round a 64th of the range
+        int lo = 0, len = n;                                     // boundaries lo .. lo + len - 1 are candidates, kept[lo] <= r0
+        while (len > 1) {
+            const int step = (len + 63) / 64;
+            const int i = lane * step;
+            const bool below = i < len && kept[lo + i] <= r0;
+            const unsigned long long m = __ballot(below);
+            const int at = (63 - __clzll((long long)(m | 1ull))) * step;
+            lo += at;
+            len = min(step, len - at);
+        }
+        // a row lies in one of the next 64 chunks, or behind them all in the tail
+        if (tid <= LC_ER_ROWS) bound_sh[tid] = lo + tid < n ? kept[lo + tid] : 0x7fffffff;
+        __syncthreads();
+        if (tid < LC_ER_ROWS) {
+            const int r = r0 + tid;
+            int row = last + (r - n_kept);
+            if (r < n_kept) {
+                int i = 0;
+    #pragma unroll
+                for (int s = 32; s > 0; s >>= 1)
+                    if (bound_sh[i + s] <= r) i += s;
+                const int id = max(0, min(ids[lo + i], M - 1));
+                row = bnd[id] + (r - bound_sh[i]);
+            }
+            row_sh[tid] = max(0, min(row, T - 1));
+        }
+        __syncthreads();
+        const int m = min(LC_ER_ROWS, rows - r0);
+        using Piece = typename std::conditional<BYTES % 16 == 0, uint4, uint32_t>::type;
+        constexpr int PIECES = BYTES / (int)sizeof(Piece);
+        const size_t from = (size_t)b * a.seq + (size_t)h * a.head, to = (size_t)b * a.seq_to + (size_t)h * a.head_to;
+        for (int i = tid; i < m * PIECES; i += LC_ER_THREADS) {
+            const int r = i / PIECES, c = i % PIECES;
+            const size_t f = from + (size_t)row_sh[r] * a.tok + c * sizeof(Piece), t = to + (size_t)(r0 + r) * a.tok_to + c * sizeof(Piece);
+            const Piece k = *reinterpret_cast<const Piece*>(a.K + f), v = *reinterpret_cast<const Piece*>(a.V + f);
+            *reinterpret_cast<Piece*>(a.K_to + t) = k;
+            *reinterpret_cast<Piece*>(a.V_to + t) = v;
+        }
+        __syncthreads();                                     // (the lists have been used)
+    }
+}
+
+// ---------------------------------------------------------------- arguments
+bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+int check_strides16(const int64_t s[3]) {
+    if (!s) return LC_ERR_INVALID_ARG;
+    for (int i = 0; i < 3; ++i)
+        if (s[i] < 0 || s[i] % 8 != 0) return LC_ERR_BAD_SHAPE;
+    return s[2] < LC_HEAD_DIM ? LC_ERR_BAD_SHAPE : LC_OK;
+}
+
+int weigh(const lc_index* idx, const void* q, const void* K, const int64_t s[3], bool in4, const int32_t* chunk_ids, const int32_t* counts, int cap,
+          int H_q, const float* lse, float* weights, void* stream) {
+    if (!idx || !q) return LC_ERR_INVALID_ARG;
+    if (H_q < idx->H_kv || H_q % idx->H_kv != 0 || H_q / idx->H_kv > LC_MAX_GROUP) return LC_ERR_BAD_SHAPE;
+    if (cap < 1 || !K || !chunk_ids || !counts || !lse || !weights) return LC_ERR_INVALID_ARG;
+    const int rc = in4 ? lc_check_strides4(s) : check_strides16(s);
+    if (rc) return rc;
+    if (!aligned(q, 16) || !aligned(K, in4 ? 4 : 16)) return LC_ERR_INVALID_ARG;
+    const int cell = in4 ? 1 : 2;
+    if ((long long)idx->cfg.max_tokens * s[2] * cell >= (1LL << 31) - 512) return LC_ERR_BAD_SHAPE;
+    LcWeighArgs a;
+    a.ix = idx->dev;
+    a.q = static_cast<const uint16_t*>(q);
+    a.K = K;
+    a.seq = s[0] * cell; a.head = s[1] * cell; a.tok = (int)(s[2] * cell);
+    a.max_tokens = idx->cfg.max_tokens;
+    a.ids = chunk_ids;
+    a.counts = counts;
+    a.cap = cap;
+    a.lse = lse;
+    a.weights = weights;
+    return in4 ? launch_weigh<true>(a, H_q / idx->H_kv, static_cast<hipStream_t>(stream)) : launch_weigh<false>(a, H_q / idx->H_kv, static_cast<hipStream_t>(stream));
+}
+
+int evict_rows(const lc_index* idx, const int32_t* keep_ids, const int32_t* keep_bounds, const int32_t* keep_counts, const void* K, const void* V,
+               const int64_t s[3], void* K_to, void* V_to, const int64_t s_to[3], bool in4, const float* weights, float* weights_to, void* stream) {
+    if (!idx || !keep_ids || !keep_bounds || !keep_counts || !K || !V || !K_to || !V_to) return LC_ERR_INVALID_ARG;
+    if ((weights != nullptr) != (weights_to != nullptr)) return LC_ERR_INVALID_ARG;
+    int rc = in4 ? lc_check_strides4(s) : check_strides16(s);
+    if (rc == LC_OK) rc = in4 ? lc_check_strides4(s_to) : check_strides16(s_to);
+    if (rc) return rc;
+    const uintptr_t al = in4 ? 4 : 16;
+    if (!aligned(K, al) || !aligned(V, al) || !aligned(K_to, al) || !aligned(V_to, al)) return LC_ERR_INVALID_ARG;
+    if (K == K_to || V == V_to || K == V_to || V == K_to || K_to == V_to || (weights && weights == weights_to)) return LC_ERR_INVALID_ARG;
+    const int cell = in4 ? 1 : 2;
+    LcEvictRowsArgs a;
+    a.ix = idx->dev;
+    a.ids = keep_ids; a.bounds = keep_bounds; a.counts = keep_counts;
+    a.K = static_cast<const char*>(K); a.V = static_cast<const char*>(V);
+    a.K_to = static_cast<char*>(K_to); a.V_to = static_cast<char*>(V_to);
+    a.seq = s[0] * cell; a.head = s[1] * cell; a.tok = s[2] * cell;
+    a.seq_to = s_to[0] * cell; a.head_to = s_to[1] * cell; a.tok_to = s_to[2] * cell;
+    a.weights = weights; a.weights_to = weights_to;
+    a.max_tokens = idx->cfg.max_tokens;
+    int most = 0;
+    for (int b = 0; b < idx->B; ++b)
+        if (idx->T[b] > most) most = idx->T[b];
+    a.row_tiles = most > 0 ? (most + LC_ER_ROWS - 1) / LC_ER_ROWS : 1;
+    const int weight_tiles = weights ? (idx->cfg.max_chunks + LC_ER_THREADS - 1) / LC_ER_THREADS : 0;
+    const dim3 grid(a.row_tiles + weight_tiles, idx->H_kv, idx->B);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (in4) hipLaunchKernelGGL(lc_evict_rows_kernel<LC_ROW4>, grid, dim3(LC_ER_THREADS), 0, st, a);
+    else hipLaunchKernelGGL(lc_evict_rows_kernel<2 * LC_D>, grid, dim3(LC_ER_THREADS), 0, st, a);
+    LC_HIP_CHECK(hipGetLastError());
+    return LC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int lc_weigh_chunks(const lc_index* idx, const void* q, const void* K, const int64_t k_strides[3], const int32_t* chunk_ids, const int32_t* counts,
+                    int cap, int H_q, const float* lse, float* weights, void* stream) {
+    return weigh(idx, q, K, k_strides, false, chunk_ids, counts, cap, H_q, lse, weights, stream);
+}
+
+int lc_weigh_chunks4(const lc_index* idx, const void* q, const void* K4, const int64_t strides4[3], const int32_t* chunk_ids, const int32_t* counts,
+                     int cap, int H_q, const float* lse, float* weights, void* stream) {
+    return weigh(idx, q, K4, strides4, true, chunk_ids, counts, cap, H_q, lse, weights, stream);
+}
+
+int lc_evict_select(const lc_index* idx, const float* weights, int keep_tokens, int recent_tokens, int32_t* keep_ids, int32_t* keep_bounds,
+                    int32_t* keep_counts, int32_t* keep_lens, void* ws, size_t ws_bytes, void* stream) {
+    if (!idx || !weights || !keep_ids || !keep_bounds || !keep_counts || !ws || !aligned(ws, 256)) return LC_ERR_INVALID_ARG;
+    if (keep_tokens < 0 || recent_tokens < 0) return LC_ERR_INVALID_ARG;
+    const size_t need = (size_t)idx->B * idx->cfg.max_chunks * sizeof(unsigned long long);
+    if (ws_bytes < need) return LC_ERR_WORKSPACE_TOO_SMALL;
+    unsigned long long* keys = static_cast<unsigned long long*>(ws);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    int most = 0;
+    for (int b = 0; b < idx->B; ++b)
+        if (idx->M[b] > most) most = idx->M[b];
+    hipLaunchKernelGGL(lc_evict_keys_kernel, dim3(most > 0 ? (most + 255) / 256 : 1, idx->B), dim3(256), 0, st, idx->dev, weights, keys);
+    LC_HIP_CHECK(hipGetLastError());
+    LcEvictArgs a;
+    a.ix = idx->dev;
+    a.keys = keys;
+    a.ids = keep_ids; a.bounds = keep_bounds; a.counts = keep_counts; a.lens = keep_lens;
+    a.keep = keep_tokens; a.recent = recent_tokens; a.sink = idx->cfg.sink_tokens;
+    hipLaunchKernelGGL(lc_evict_select_kernel, dim3(idx->B), dim3(LC_EV_THREADS), 0, st, a);
+    LC_HIP_CHECK(hipGetLastError());
+    return LC_OK;
+}
+
+int lc_evict_rows(const lc_index* idx, const int32_t* keep_ids, const int32_t* keep_bounds, const int32_t* keep_counts, const void* K, const void* V,
+                  const int64_t kv_strides[3], void* K_to, void* V_to, const int64_t to_strides[3], const float* weights, float* weights_to, void* stream) {
+    return evict_rows(idx, keep_ids, keep_bounds, keep_counts, K, V, kv_strides, K_to, V_to, to_strides, false, weights, weights_to, stream);
+}
+
+int lc_evict_rows4(const lc_index* idx, const int32_t* keep_ids, const int32_t* keep_bounds, const int32_t* keep_counts, const void* K4, const void* V4,
+                   const int64_t strides4[3], void* K4_to, void* V4_to, const int64_t to_strides4[3], const float* weights, float* weights_to, void* stream) {
+    return evict_rows(idx, keep_ids, keep_bounds, keep_counts, K4, V4, strides4, K4_to, V4_to, to_strides4, true, weights, weights_to, stream);
+}
+
+}  // extern "C"

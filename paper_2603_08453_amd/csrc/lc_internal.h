@@ -132,6 +132,9 @@ extern "C" int lc_recluster_impl(lc_index* idx, void* ws, size_t ws_bytes, void*
 int lc_walk_max_internal_nodes();   // exact walk: internal nodes of one (sequence, head), all levels together
 int lc_beam_max_level_nodes();      // top-k per level: nodes of one internal level of one (sequence, head)
 
+// Strides {sequence, head, token} in bytes of a cache in 4 bits.
+int lc_check_strides4(const int64_t s[3]);
+
 // Launchers (each enqueues on `stream` and returns LC_OK or LC_ERR_HIP).
 int lc_launch_build(const lc_index* idx, const LcWs& ws, const void* K, const int64_t ks[3],
                     int max_M, hipStream_t stream);
@@ -168,3 +171,6 @@ int lc_launch_place_counts(const lc_index* idx, const int32_t* staged, hipStream
 int lc_launch_append(const lc_index* idx, void* K, void* V, const int64_t ks[3],
                      const void* k_new, const void* v_new, const uint8_t* close_dev_flags_or_null,
                      uint32_t close_mask_lo, hipStream_t stream);
+// The same over a cache in 4 bits, strides in bytes.
+int lc_launch_append4(const lc_index* idx, void* K4, void* V4, const int64_t strides4[3],
+                      const void* k_new, const void* v_new, const uint8_t* close_chunk, hipStream_t stream);
