@@ -191,6 +191,7 @@ class _Unmarshalled:
         return NotImplemented
 
     decode_step = retrieve = sparse_decode = append = _pass
+    move4 = sparse_decode4 = append4 = weigh_chunks = evict_select = evict_rows = _pass
 
 
 def _fast():
@@ -208,6 +209,9 @@ def _fast():
             return _fast_mod
         _lychee_torch.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in
                              (L.lc_decode_step, L.lc_decode_step_static, L.lc_retrieve, L.lc_sparse_decode, L.lc_append)))
+        _lychee_torch.bind4(*(ctypes.cast(f, ctypes.c_void_p).value for f in
+                              (L.lc_cache4_store, L.lc_cache4_load, L.lc_sparse_decode4, L.lc_append4, L.lc_weigh_chunks, L.lc_weigh_chunks4,
+                               L.lc_evict_select, L.lc_evict_rows, L.lc_evict_rows4)))
         _fast_mod = _lychee_torch
     return _fast_mod
 
@@ -464,7 +468,18 @@ def _strides4(t) -> "ctypes.Array":
     return (ctypes.c_int64 * 3)(t.stride(0), t.stride(1), t.stride(2))
 
 
+def _done(rc, where: str) -> bool:
+    """Whether the native module made the call; raises if the library refused it."""
+    if rc is NotImplemented:
+        return False
+    if rc:
+        raise LycheeError(rc, where)
+    return True
+
+
 def _move4(call, where, K, V, K4, V4, first, counts, stream, store):
+    if _done((_fast_mod or _fast()).move4(store, K, V, K4, V4, first, counts, stream), where):
+        return
     B, H_kv, rows, d = K.shape
     assert K.shape == V.shape and K.stride() == V.stride() and K4.shape == V4.shape and K4.stride() == V4.stride()
     assert K4.shape[:2] == K.shape[:2] and K.element_size() == 2
@@ -488,6 +503,8 @@ def lc_cache4_load(K4, V4, K, V, first=None, counts=None, stream=None) -> None:
 
 def lc_sparse_decode4(idx: Index, q, K4, V4, chunk_ids, counts, out, ws, lse=None, stream=None) -> None:
     """lc_sparse_decode over a 4-bit cache (uint8 [B][H_kv][tokens][68])."""
+    if _done((_fast_mod or _fast()).sparse_decode4(idx.address, q, K4, V4, chunk_ids, counts, out, ws, lse, stream), "lc_sparse_decode4"):
+        return
     assert K4.stride() == V4.stride()
     _check(lib().lc_sparse_decode4(idx.handle, _ptr(q), _ptr(K4), _ptr(V4), _strides4(K4), _ptr(chunk_ids), _ptr(counts),
                                    chunk_ids.shape[2], q.shape[1], _ptr(out), _ptr(lse), _ptr(ws), ws.numel() * ws.element_size(),
@@ -496,6 +513,8 @@ def lc_sparse_decode4(idx: Index, q, K4, V4, chunk_ids, counts, out, ws, lse=Non
 
 def lc_append4(idx: Index, K4, V4, k_new, v_new, close_chunk: Optional[Sequence[int]] = None, stream=None) -> None:
     """lc_append over a 4-bit cache."""
+    if _done((_fast_mod or _fast()).append4(idx.address, K4, V4, k_new, v_new, close_chunk, stream), "lc_append4"):
+        return
     cc = None
     if close_chunk is not None:
         cc = (ctypes.c_uint8 * len(close_chunk))(*[1 if c else 0 for c in close_chunk])
@@ -507,12 +526,16 @@ def lc_append4(idx: Index, K4, V4, k_new, v_new, close_chunk: Optional[Sequence[
 
 def lc_weigh_chunks(idx: Index, q, K, chunk_ids, counts, lse, weights, stream=None) -> None:
     """Adds each listed chunk's attention weight to weights (float32 [B][H_kv][max_chunks]); lse float32 [B][H_q] as lc_sparse_decode gives it."""
+    if _done((_fast_mod or _fast()).weigh_chunks(idx.address, q, K, chunk_ids, counts, lse, weights, stream, False), "lc_weigh_chunks"):
+        return
     _check(lib().lc_weigh_chunks(idx.handle, _ptr(q), _ptr(K), _strides3(K), _ptr(chunk_ids), _ptr(counts), chunk_ids.shape[2], q.shape[1],
                                  _ptr(lse), _ptr(weights), _stream(stream)), "lc_weigh_chunks")
 
 
 def lc_weigh_chunks4(idx: Index, q, K4, chunk_ids, counts, lse, weights, stream=None) -> None:
     """lc_weigh_chunks over a 4-bit cache."""
+    if _done((_fast_mod or _fast()).weigh_chunks(idx.address, q, K4, chunk_ids, counts, lse, weights, stream, True), "lc_weigh_chunks4"):
+        return
     _check(lib().lc_weigh_chunks4(idx.handle, _ptr(q), _ptr(K4), _strides4(K4), _ptr(chunk_ids), _ptr(counts), chunk_ids.shape[2], q.shape[1],
                                   _ptr(lse), _ptr(weights), _stream(stream)), "lc_weigh_chunks4")
 
@@ -520,12 +543,17 @@ def lc_weigh_chunks4(idx: Index, q, K4, chunk_ids, counts, lse, weights, stream=
 def lc_evict_select(idx: Index, weights, keep_tokens: int, recent_tokens: int, keep_ids, keep_bounds, keep_counts, ws, keep_lens=None,
                     stream=None) -> None:
     """keep_ids int32 [B][max_chunks], keep_bounds int32 [B][max_chunks + 1], keep_counts int32 [B], keep_lens int32 [B] or None."""
+    if _done((_fast_mod or _fast()).evict_select(idx.address, weights, keep_tokens, recent_tokens, keep_ids, keep_bounds, keep_counts, ws, keep_lens, stream),
+             "lc_evict_select"):
+        return
     _check(lib().lc_evict_select(idx.handle, _ptr(weights), int(keep_tokens), int(recent_tokens), _ptr(keep_ids), _ptr(keep_bounds),
                                  _ptr(keep_counts), _ptr(keep_lens), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)), "lc_evict_select")
 
 
 def lc_evict_rows(idx: Index, keep_ids, keep_bounds, keep_counts, K, V, K_to, V_to, weights=None, weights_to=None, stream=None) -> None:
     """The kept chunks' rows and the open tail's from K and V to the front of K_to and V_to; bf16 caches, or 4-bit ones (uint8)."""
+    if _done((_fast_mod or _fast()).evict_rows(idx.address, keep_ids, keep_bounds, keep_counts, K, V, K_to, V_to, weights, weights_to, stream), "lc_evict_rows"):
+        return
     assert K.stride() == V.stride() and K_to.stride() == V_to.stride() and K.element_size() == K_to.element_size()
     call, strides = (lib().lc_evict_rows4, _strides4) if K.element_size() == 1 else (lib().lc_evict_rows, _strides3)
     _check(call(idx.handle, _ptr(keep_ids), _ptr(keep_bounds), _ptr(keep_counts), _ptr(K), _ptr(V), strides(K), _ptr(K_to), _ptr(V_to),

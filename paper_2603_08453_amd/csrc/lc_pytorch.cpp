@@ -21,6 +21,34 @@ decltype(&lc_decode_step_static) g_decode_step_static = nullptr;
 decltype(&lc_retrieve) g_retrieve = nullptr;
 decltype(&lc_sparse_decode) g_sparse_decode = nullptr;
 decltype(&lc_append) g_append = nullptr;
+decltype(&lc_cache4_store) g_cache4_store = nullptr;
+decltype(&lc_cache4_load) g_cache4_load = nullptr;
+decltype(&lc_sparse_decode4) g_sparse_decode4 = nullptr;
+decltype(&lc_append4) g_append4 = nullptr;
+decltype(&lc_weigh_chunks) g_weigh_chunks = nullptr;
+decltype(&lc_weigh_chunks4) g_weigh_chunks4 = nullptr;
+decltype(&lc_evict_select) g_evict_select = nullptr;
+decltype(&lc_evict_rows) g_evict_rows = nullptr;
+decltype(&lc_evict_rows4) g_evict_rows4 = nullptr;
+
+// The entry points of the 4-bit cache and of the eviction.
+PyObject* bind4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (n != 9) {
+        PyErr_SetString(PyExc_TypeError, "bind4(cache4_store, cache4_load, sparse_decode4, append4, weigh_chunks, weigh_chunks4, evict_select, evict_rows, evict_rows4)");
+        return nullptr;
+    }
+    g_cache4_store = reinterpret_cast<decltype(g_cache4_store)>(PyLong_AsVoidPtr(a[0]));
+    g_cache4_load = reinterpret_cast<decltype(g_cache4_load)>(PyLong_AsVoidPtr(a[1]));
+    g_sparse_decode4 = reinterpret_cast<decltype(g_sparse_decode4)>(PyLong_AsVoidPtr(a[2]));
+    g_append4 = reinterpret_cast<decltype(g_append4)>(PyLong_AsVoidPtr(a[3]));
+    g_weigh_chunks = reinterpret_cast<decltype(g_weigh_chunks)>(PyLong_AsVoidPtr(a[4]));
+    g_weigh_chunks4 = reinterpret_cast<decltype(g_weigh_chunks4)>(PyLong_AsVoidPtr(a[5]));
+    g_evict_select = reinterpret_cast<decltype(g_evict_select)>(PyLong_AsVoidPtr(a[6]));
+    g_evict_rows = reinterpret_cast<decltype(g_evict_rows)>(PyLong_AsVoidPtr(a[7]));
+    g_evict_rows4 = reinterpret_cast<decltype(g_evict_rows4)>(PyLong_AsVoidPtr(a[8]));
+    if (PyErr_Occurred()) return nullptr;
+    Py_RETURN_NONE;
+}
 
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (n != 5) {
@@ -213,6 +241,22 @@ PyObject* sparse_decode(PyObject*, PyObject* const* args, Py_ssize_t n) {
     });
 }
 
+// The close flags of an append: truth values of a sized iterable.
+bool close_flags(PyObject* given, uint8_t (&flags)[1024]) {
+    // (a tuple of its own: telling whether an element is true can run code that changes the caller's list)
+    PyObject* const seq = PyObject_Size(given) >= 0 ? PySequence_Tuple(given) : nullptr;
+    if (!seq) return false;
+    const Py_ssize_t m = PyTuple_GET_SIZE(seq);
+    bool ok = m <= (Py_ssize_t)sizeof(flags);
+    for (Py_ssize_t i = 0; ok && i < m; ++i) {
+        const int t = PyObject_IsTrue(PyTuple_GET_ITEM(seq, i));
+        if (t < 0) ok = false;
+        else flags[i] = (uint8_t)t;
+    }
+    Py_DECREF(seq);
+    return ok;
+}
+
 // append(handle, K, V, k_new, v_new, close flags or None, ws, stream)
 PyObject* append(PyObject*, PyObject* const* args, Py_ssize_t n) {
     Args a(args, n);
@@ -224,20 +268,7 @@ PyObject* append(PyObject*, PyObject* const* args, Py_ssize_t n) {
         if (!cache_strides(*K, *V, false, s)) return true;
         uint8_t flags[1024] = {};                            // lc_append takes at most 1024 sequences
         const bool given = a[5] != Py_None;
-        if (given) {
-            // (a tuple of its own: telling whether an element is true can run code that changes the caller's list)
-            PyObject* const seq = PyObject_Size(a[5]) >= 0 ? PySequence_Tuple(a[5]) : nullptr;
-            if (!seq) return false;
-            const Py_ssize_t m = PyTuple_GET_SIZE(seq);
-            bool ok = m <= (Py_ssize_t)sizeof(flags);
-            for (Py_ssize_t i = 0; ok && i < m; ++i) {
-                const int t = PyObject_IsTrue(PyTuple_GET_ITEM(seq, i));
-                if (t < 0) ok = false;
-                else flags[i] = (uint8_t)t;
-            }
-            Py_DECREF(seq);
-            if (!ok) return false;
-        }
+        if (given && !close_flags(a[5], flags)) return false;
         void* const st = a.stream(7);
         if (PyErr_Occurred()) return false;
         lc_index* const idx = a.handle(0);
@@ -252,6 +283,207 @@ PyObject* append(PyObject*, PyObject* const* args, Py_ssize_t n) {
     });
 }
 
+// Strides of a 4-bit cache, in bytes.
+bool cache4_strides(const at::Tensor& K4, const at::Tensor& V4, int64_t (&s)[3]) {
+    if (!K4.strides().equals(V4.strides())) {
+        PyErr_SetString(PyExc_AssertionError, "K4 and V4 must have the same strides");
+        return false;
+    }
+    if (K4.dim() != 4 || K4.size(3) != LC_CACHE4_ROW || K4.stride(3) != 1 || K4.element_size() != 1) {
+        PyErr_SetString(PyExc_AssertionError, "4-bit cache must be uint8 [B][H_kv][tokens][68] with a row's bytes contiguous");
+        return false;
+    }
+    for (int i = 0; i < 3; ++i) s[i] = K4.stride(i);
+    return true;
+}
+// At most N whole numbers of a sequence into `to`; false without a Python error: not ours.
+template <size_t N>
+bool numbers(PyObject* given, Py_ssize_t n, int32_t (&to)[N]) {
+    PyObject* const seq = PySequence_Tuple(given);
+    if (!seq) { PyErr_Clear(); return false; }
+    bool ok = PyTuple_GET_SIZE(seq) == n && n <= (Py_ssize_t)N;
+    for (Py_ssize_t i = 0; ok && i < n; ++i) {
+        const long v = PyLong_AsLong(PyTuple_GET_ITEM(seq, i));
+        ok = !PyErr_Occurred() && v >= -0x7fffffffL && v <= 0x7fffffffL;
+        to[i] = (int32_t)v;
+    }
+    PyErr_Clear();
+    Py_DECREF(seq);
+    return ok;
+}
+
+// move4(store, K, V, K4, V4, first or None, counts or None, stream): lc_cache4_store or lc_cache4_load.  What is unusual (a wrong shape among it)
+// is left to the binding's own route.
+PyObject* move4(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    Args a(args, n);
+    if (!a.count(8)) return nullptr;
+    return guarded(a, [&](int* rc) {
+        const bool store = a[0] == Py_True;
+        const at::Tensor *K = a.tensor(1), *V = a.tensor(2), *K4 = a.tensor(3), *V4 = a.tensor(4);
+        if (!K || !V || !K4 || !V4 || a.foreign()) return false;
+        if (K->dim() != 4 || K4->dim() != 4 || K->element_size() != 2 || !K->sizes().equals(V->sizes()) || !K4->sizes().equals(V4->sizes()) ||
+            K->size(0) != K4->size(0) || K->size(1) != K4->size(1) || K->size(0) > 256 || K->size(2) > 0x7fffffffL || K4->size(2) > 0x7fffffffL)
+            return false;
+        int64_t s[3], s4[3];
+        if (!cache_strides(*K, *V, true, s) || !cache4_strides(*K4, *V4, s4)) return true;
+        const int B = (int)K->size(0), H = (int)K->size(1), rows = (int)K->size(2), d = (int)K->size(3);
+        int32_t first[256], counts[256];
+        const bool given = a[5] != Py_None;
+        if (given && !numbers(a[5], B, first)) return false;
+        if (a[6] == Py_None) {
+            for (int b = 0; b < B; ++b) counts[b] = rows;
+        } else if (!numbers(a[6], B, counts)) {
+            return false;
+        }
+        for (int b = 0; b < B; ++b)
+            if (counts[b] > rows) return false;
+        void* const st = a.stream(7);
+        if (PyErr_Occurred()) return false;
+        void *kd = K->data_ptr(), *vd = V->data_ptr(), *k4 = K4->data_ptr(), *v4 = V4->data_ptr();
+        const int cap = (int)K4->size(2);
+        const Unlocked unlocked;
+        *rc = store ? g_cache4_store(kd, vd, s, given ? first : nullptr, counts, B, H, d, k4, v4, s4, cap, st)
+                    : g_cache4_load(k4, v4, s4, given ? first : nullptr, counts, B, H, d, kd, vd, s, cap, st);
+        return true;
+    });
+}
+
+// sparse_decode4(handle, q, K4, V4, chunk_ids, counts, out, ws, lse, stream)
+PyObject* sparse_decode4(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    Args a(args, n);
+    if (!a.count(10)) return nullptr;
+    return guarded(a, [&](int* rc) {
+        const at::Tensor *q = a.tensor(1), *K = a.tensor(2), *V = a.tensor(3), *ids = a.tensor(4), *ws = a.tensor(7);
+        if (!q || !K || !V || !ids || !ws || a.foreign()) return false;
+        int64_t s[3];
+        if (!cache4_strides(*K, *V, s)) return true;
+        const int32_t* const counts = static_cast<const int32_t*>(a.ptr(5));
+        float* const out = static_cast<float*>(a.ptr(6));
+        float* const lse = static_cast<float*>(a.ptr(8));
+        if (a.foreign()) return false;
+        void* const st = a.stream(9);
+        if (PyErr_Occurred()) return false;
+        lc_index* const idx = a.handle(0);
+        if (PyErr_Occurred()) return false;
+        const void *qd = q->data_ptr(), *kd = K->data_ptr(), *vd = V->data_ptr();
+        const int32_t* const idp = static_cast<const int32_t*>(ids->data_ptr());
+        const int H_q = (int)q->size(1), cap = (int)ids->size(2);
+        void* const wd = ws->data_ptr();
+        const size_t wn = bytes(*ws);
+        const Unlocked unlocked;
+        *rc = g_sparse_decode4(idx, qd, kd, vd, s, idp, counts, cap, H_q, out, lse, wd, wn, st);
+        return true;
+    });
+}
+
+// append4(handle, K4, V4, k_new, v_new, close flags or None, stream)
+PyObject* append4(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    Args a(args, n);
+    if (!a.count(7)) return nullptr;
+    return guarded(a, [&](int* rc) {
+        const at::Tensor *K = a.tensor(1), *V = a.tensor(2), *k = a.tensor(3), *v = a.tensor(4);
+        if (!K || !V || !k || !v || a.foreign()) return false;
+        int64_t s[3];
+        if (!cache4_strides(*K, *V, s)) return true;
+        uint8_t flags[1024] = {};                            // lc_append4 takes at most 1024 sequences
+        const bool given = a[5] != Py_None;
+        if (given && !close_flags(a[5], flags)) return false;
+        void* const st = a.stream(6);
+        if (PyErr_Occurred()) return false;
+        lc_index* const idx = a.handle(0);
+        if (PyErr_Occurred()) return false;
+        void *kd = K->data_ptr(), *vd = V->data_ptr();
+        const void *kn = k->data_ptr(), *vn = v->data_ptr();
+        const Unlocked unlocked;
+        *rc = g_append4(idx, kd, vd, s, kn, vn, given ? flags : nullptr, st);
+        return true;
+    });
+}
+
+// weigh_chunks(handle, q, K or K4, chunk_ids, counts, lse, weights, stream, in 4 bits)
+PyObject* weigh_chunks(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    Args a(args, n);
+    if (!a.count(9)) return nullptr;
+    return guarded(a, [&](int* rc) {
+        const at::Tensor *q = a.tensor(1), *K = a.tensor(2), *ids = a.tensor(3);
+        const bool in4 = a[8] == Py_True;
+        if (!q || !K || !ids || a.foreign()) return false;
+        int64_t s[3];
+        if (in4 ? !cache4_strides(*K, *K, s) : !cache_strides(*K, *K, false, s)) return true;
+        const int32_t* const counts = static_cast<const int32_t*>(a.ptr(4));
+        const float* const lse = static_cast<const float*>(a.ptr(5));
+        float* const weights = static_cast<float*>(a.ptr(6));
+        if (a.foreign()) return false;
+        void* const st = a.stream(7);
+        if (PyErr_Occurred()) return false;
+        lc_index* const idx = a.handle(0);
+        if (PyErr_Occurred()) return false;
+        const void *qd = q->data_ptr(), *kd = K->data_ptr();
+        const int32_t* const idp = static_cast<const int32_t*>(ids->data_ptr());
+        const int H_q = (int)q->size(1), cap = (int)ids->size(2);
+        const Unlocked unlocked;
+        *rc = (in4 ? g_weigh_chunks4 : g_weigh_chunks)(idx, qd, kd, s, idp, counts, cap, H_q, lse, weights, st);
+        return true;
+    });
+}
+
+// evict_select(handle, weights, keep_tokens, recent_tokens, keep_ids, keep_bounds, keep_counts, ws, keep_lens, stream)
+PyObject* evict_select(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    Args a(args, n);
+    if (!a.count(10)) return nullptr;
+    return guarded(a, [&](int* rc) {
+        const at::Tensor *w = a.tensor(1), *ws = a.tensor(7);
+        if (!w || !ws || a.foreign()) return false;
+        const int keep = a.integer(2), recent = a.integer(3);
+        if (PyErr_Occurred()) return false;
+        int32_t* const ids = static_cast<int32_t*>(a.ptr(4));
+        int32_t* const bounds = static_cast<int32_t*>(a.ptr(5));
+        int32_t* const counts = static_cast<int32_t*>(a.ptr(6));
+        int32_t* const lens = static_cast<int32_t*>(a.ptr(8));
+        if (a.foreign()) return false;
+        void* const st = a.stream(9);
+        if (PyErr_Occurred()) return false;
+        lc_index* const idx = a.handle(0);
+        if (PyErr_Occurred()) return false;
+        const float* const wd = static_cast<const float*>(w->data_ptr());
+        void* const sd = ws->data_ptr();
+        const size_t sn = bytes(*ws);
+        const Unlocked unlocked;
+        *rc = g_evict_select(idx, wd, keep, recent, ids, bounds, counts, lens, sd, sn, st);
+        return true;
+    });
+}
+
+// evict_rows(handle, keep_ids, keep_bounds, keep_counts, K, V, K_to, V_to, weights, weights_to, stream)
+PyObject* evict_rows(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    Args a(args, n);
+    if (!a.count(11)) return nullptr;
+    return guarded(a, [&](int* rc) {
+        const at::Tensor *K = a.tensor(4), *V = a.tensor(5), *K_to = a.tensor(6), *V_to = a.tensor(7);
+        if (!K || !V || !K_to || !V_to || a.foreign()) return false;
+        const bool in4 = K->element_size() == 1;
+        int64_t s[3], st_to[3];
+        if (K->element_size() != K_to->element_size()) return false;
+        if (in4 ? !cache4_strides(*K, *V, s) || !cache4_strides(*K_to, *V_to, st_to) : !cache_strides(*K, *V, false, s) || !cache_strides(*K_to, *V_to, false, st_to))
+            return true;
+        const int32_t* const ids = static_cast<const int32_t*>(a.ptr(1));
+        const int32_t* const bounds = static_cast<const int32_t*>(a.ptr(2));
+        const int32_t* const counts = static_cast<const int32_t*>(a.ptr(3));
+        const float* const w = static_cast<const float*>(a.ptr(8));
+        float* const w_to = static_cast<float*>(a.ptr(9));
+        if (a.foreign()) return false;
+        void* const st = a.stream(10);
+        if (PyErr_Occurred()) return false;
+        lc_index* const idx = a.handle(0);
+        if (PyErr_Occurred()) return false;
+        const void *kd = K->data_ptr(), *vd = V->data_ptr();
+        void *kt = K_to->data_ptr(), *vt = V_to->data_ptr();
+        const Unlocked unlocked;
+        *rc = (in4 ? g_evict_rows4 : g_evict_rows)(idx, ids, bounds, counts, kd, vd, s, kt, vt, st_to, w, w_to, st);
+        return true;
+    });
+}
+
 template <typename F>
 PyCFunction fast(F f) { return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)); }
 
@@ -261,6 +493,13 @@ PyMethodDef methods[] = {
     {"retrieve", fast(retrieve), METH_FASTCALL, ""},
     {"sparse_decode", fast(sparse_decode), METH_FASTCALL, ""},
     {"append", fast(append), METH_FASTCALL, ""},
+    {"bind4", fast(bind4), METH_FASTCALL, "addresses of the 4-bit cache's and the eviction's entry points"},
+    {"move4", fast(move4), METH_FASTCALL, ""},
+    {"sparse_decode4", fast(sparse_decode4), METH_FASTCALL, ""},
+    {"append4", fast(append4), METH_FASTCALL, ""},
+    {"weigh_chunks", fast(weigh_chunks), METH_FASTCALL, ""},
+    {"evict_select", fast(evict_select), METH_FASTCALL, ""},
+    {"evict_rows", fast(evict_rows), METH_FASTCALL, ""},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lychee_torch", "Tensor marshalling of the per-token entry points.", -1,
                       methods, nullptr, nullptr, nullptr, nullptr};
