@@ -21,7 +21,8 @@
 #define LC_C4_BATCH 64            // sequences of a launch: their row numbers are launch arguments
 #define LC_D4_THREADS 256
 #define LC_D4_WAVES (LC_D4_THREADS / 64)
-#define LC_D4_TILE 1024           // tokens of a split whose cache rows are resolved into LDS at a time
+#define LC_D4_TILE 8192           // tokens of a split whose cache rows are resolved into LDS at a time
+#define LC_D4_MIN_TOKENS 128      // tokens of a split, at least: a step of each wavefront (8 heads of 1024 tokens: 8.7 us, with 64 9.0, with 256 9.4; of 2048: 8.9, 9.7, 9.5)
 #define LC_D4_E 8                 // listed chunks per thread and pass of the row resolution
 #define LC_D4_MAX_SPLITS 256
 #define LC_LOG2E 1.4426950408889634f
@@ -122,6 +123,7 @@ lc_decode4_kernel(const LcDecode4Args a) {
     constexpr int COLS = WIDE ? 16 : 3 * G;      // columns that hold something
     constexpr int TERMS = WIDE ? 2 : 3;          // columns of a head
     constexpr int STEP = 32;
+    constexpr int E = LC_D4_E, PASS = E * LC_D4_THREADS;
     constexpr int ROW = LC_D + 4;                // floats between the columns' sums in LDS: lanes of different columns use different banks
     union Phases {
         struct {
@@ -129,29 +131,32 @@ lc_decode4_kernel(const LcDecode4Args a) {
             float ml[LC_D4_WAVES][G][2];
         } comb;
         struct {
-            float m[LC_MAX_GROUP * LC_D4_MAX_SPLITS], l[LC_MAX_GROUP * LC_D4_MAX_SPLITS];
+            float scale[LC_D4_THREADS / 32][LC_D4_MAX_SPLITS + 128], sum[LC_D4_THREADS / 32][LC_D4_MAX_SPLITS];
             float4 red[LC_D4_THREADS];
         } merge;
-        int row[LC_D4_TILE];                     // byte offsets of the cache rows of the tile's tokens
+        int row[LC_D4_TILE + 2 * LC_D4_WAVES * STEP];    // byte offsets of the cache rows of the tile's tokens
     };
     __shared__ __attribute__((aligned(16))) Phases ph;
+    __shared__ __attribute__((aligned(16))) int off_sh[E * LC_D4_THREADS + 4], st_sh[E * LC_D4_THREADS];
     __shared__ int scan_sh[8];
-    __shared__ int last_sh;
+    __shared__ int first_sh, last_sh;
 
     const LcDev& ix = a.ix;
     const int s = blockIdx.x, S = gridDim.x, h = blockIdx.y, b = blockIdx.z;
     const int bh = b * ix.H + h;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, kg = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, kg = lane >> 4;
     // the head and the term of this lane's column
     const int term = WIDE ? n >> 3 : n / G;
     const int head = WIDE ? min(n & 7, G - 1) : n - term * G;
+    // which of a probability's terms come before this column's, as masks; and whether it has one (the third, where that is apart)
+    const uint32_t past0 = term >= 1 ? 0xffff0000u : 0u, past1 = term >= 2 ? 0xffff0000u : 0u;
+    const uint32_t here = WIDE ? (term == 0 ? 0xffffffffu : 0u) : (term < 3 ? 0xffffffffu : 0u);
 
     const __amdgpu_buffer_rsrc_t bnd_r = lc_buffer(ix.bounds + (size_t)b * (ix.cap[0] + 1), (ix.cap[0] + 1) * 4);
     const __amdgpu_buffer_rsrc_t ids_r = lc_buffer(a.ids + (size_t)bh * a.cap, (int)(min((long long)a.cap, 1LL << 28) * 4));
 
     // ---- the attended tokens: the listed chunks in the list's order, then the open tail.  Thread t of a pass owns entries [E t, E t + E);
     // the first pass stays in registers.
-    constexpr int E = LC_D4_E, PASS = E * LC_D4_THREADS;
     lc_v4i idv[E / 4];
     auto load_ids = [&](int base) LC_INLINE {
 #pragma unroll
@@ -196,7 +201,7 @@ lc_decode4_kernel(const LcDecode4Args a) {
         n_sel += tot;
     }
     const int n_tok = n_sel + tail_ln;
-    const int S_eff = max(1, min(S, (n_tok + LC_DEC_MIN_TOKENS_PER_SPLIT - 1) / LC_DEC_MIN_TOKENS_PER_SPLIT));
+    const int S_eff = max(1, min(S, (n_tok + LC_D4_MIN_TOKENS - 1) / LC_D4_MIN_TOKENS));
     if (s >= S_eff) return;                      // (the same n_tok in all of them: nobody waits for these)
 
     const float scale = 0.08838834764831845f * LC_LOG2E;     // log2(e) / sqrt(128)
@@ -256,12 +261,13 @@ lc_decode4_kernel(const LcDecode4Args a) {
         // (a whole number: scaling the sums by the difference of two rounds nothing)
         if (__ballot(mx > m_ref) != 0ull) {
             const float m_new = mx > m_ref ? ceilf(mx) : m_ref;
-            const float by = __builtin_amdgcn_exp2f(m_ref - m_new);
-            const float f = m_ref == m_new ? 1.f : by;
+            const int by = m_ref == m_new ? 0 : (int)fmaxf(m_ref - m_new, -1024.f);
             m_ref = m_new;
-            l_run *= f;
+            l_run = __builtin_ldexpf(l_run, by);
 #pragma unroll
-            for (int c = 0; c < 8; ++c) acc[c] *= f;
+            for (int c = 0; c < 8; ++c)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[c][r] = __builtin_ldexpf(acc[c][r], by);
         }
         const float ref = m_ref == LC_NEG_INF ? 0.f : m_ref;
         float p[8];
@@ -274,20 +280,21 @@ lc_decode4_kernel(const LcDecode4Args a) {
             uint32_t w0[8], w1[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float r1 = p[j] - __uint_as_float(__float_as_uint(p[j]) & 0xffff0000u);
-                const float r2 = r1 - __uint_as_float(__float_as_uint(r1) & 0xffff0000u);
+                float r = p[j];
+                r -= __uint_as_float(__float_as_uint(r) & past0);
                 if constexpr (WIDE) {
-                    w0[j] = __float_as_uint(term == 0 ? p[j] : r1);
-                    w1[j] = __float_as_uint(term == 0 ? r2 : 0.f);
+                    const float r1 = p[j] - __uint_as_float(__float_as_uint(p[j]) & 0xffff0000u);
+                    w0[j] = __float_as_uint(r);
+                    w1[j] = __float_as_uint(r1 - __uint_as_float(__float_as_uint(r1) & 0xffff0000u)) & here;
                 } else {
-                    w0[j] = __float_as_uint(term == 0 ? p[j] : term == 1 ? r1 : term == 2 ? r2 : 0.f);
-                    w1[j] = 0u;
+                    r -= __uint_as_float(__float_as_uint(r) & past1);
+                    w0[j] = __float_as_uint(r) & here;
                 }
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 t0[j] = (int)__builtin_amdgcn_perm(w0[2 * j + 1], w0[2 * j], 0x07060302u);
-                t1[j] = (int)__builtin_amdgcn_perm(w1[2 * j + 1], w1[2 * j], 0x07060302u);
+                if constexpr (WIDE) t1[j] = (int)__builtin_amdgcn_perm(w1[2 * j + 1], w1[2 * j], 0x07060302u);
             }
         }
 #pragma unroll
@@ -316,51 +323,69 @@ lc_decode4_kernel(const LcDecode4Args a) {
     };
 
     // ---- the split's tokens, in tiles whose rows the workgroup first writes into LDS
-    const int lo = (int)((long long)n_tok * s / S_eff), hi = (int)((long long)n_tok * (s + 1) / S_eff);
+    // tokens [n_tok s / S_eff, n_tok (s + 1) / S_eff), in 32 bits: with n_tok = each S_eff + more, more < S_eff <= 256
+    const uint32_t each = (uint32_t)n_tok / (uint32_t)S_eff, more = (uint32_t)n_tok % (uint32_t)S_eff;
+    const int lo = (int)(each * (uint32_t)s + more * (uint32_t)s / (uint32_t)S_eff);
+    const int hi = (int)(each * (uint32_t)(s + 1) + more * (uint32_t)(s + 1) / (uint32_t)S_eff);
     const int row_max = max(T - 1, 0);
     for (int tile0 = lo; tile0 < hi; tile0 += LC_D4_TILE) {
         const int tl = min(LC_D4_TILE, hi - tile0);
-        auto fill = [&](int o, int st, int ln) LC_INLINE {
-            const int k0 = max(o, tile0), k1 = min(o + ln, tile0 + tl);
-            for (int k = k0 + lane; k < k1; k += 64) ph.row[k - tile0] = min(st + (k - o), row_max) * a.tok;
-        };
-        // 64 lanes per chunk that overlaps the tile (its lane's values are read by number)
-        auto visit = [&](int off, const int (&st)[E], const int (&ln)[E]) LC_INLINE {
+        // The entries' places in the list go into LDS, then 16 lanes take one entry that overlaps the tile, 16 tokens at a time.
+        auto place = [&](int carry, int ex, int tot, int count, const int (&st)[E], const int (&ln)[E]) LC_INLINE {
+            if (tile0 >= carry + tot || carry >= tile0 + tl) return;
+            __syncthreads();                                        // (the entries before have been used)
+            int off = carry + ex;
+            if (tid == 0 && tile0 < carry) first_sh = 0;
+            if (tid * E < count) {
+                lc_v4i o[E / 4], f[E / 4];
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                unsigned long long mask = __ballot(ln[e] > 0 && off < tile0 + tl && tile0 < off + ln[e]);
-                while (mask != 0ull) {
-                    const int l = __ffsll((long long)mask) - 1;
-                    mask &= mask - 1ull;
-                    fill(lc_readlane(off, l), lc_readlane(st[e], l), lc_readlane(ln[e], l));
+                for (int e = 0; e < E; ++e) {
+                    o[e / 4][e % 4] = off;
+                    f[e / 4][e % 4] = st[e];
+                    if (off <= tile0 && tile0 < off + ln[e]) first_sh = tid * E + e;
+                    off += ln[e];
                 }
-                off += ln[e];
+#pragma unroll
+                for (int e = 0; e < E / 4; ++e) {
+                    reinterpret_cast<lc_v4i*>(off_sh)[tid * (E / 4) + e] = o[e];
+                    reinterpret_cast<lc_v4i*>(st_sh)[tid * (E / 4) + e] = f[e];
+                }
+                if (tid * E + E >= count) off_sh[tid * E + E] = off;
+            }
+            __syncthreads();
+            for (int i = first_sh + (tid >> 4); i < count; i += LC_D4_THREADS / 16) {
+                const int o = off_sh[i], k1 = min(off_sh[i + 1], tile0 + tl), from = st_sh[i] - o;
+                if (o >= tile0 + tl) break;
+                for (int k = max(o, tile0) + n; k < k1; k += 16) ph.row[k - tile0] = min(from + k, row_max) * a.tok;
             }
         };
         if (tile0 != lo) __syncthreads();                           // the previous tile's rows have been used
-        visit(ex0, st0, ln0);
+        place(0, ex0, tot0, min(n_ids, PASS), st0, ln0);
         int carry = tot0;
         for (int base = PASS; base < n_ids; base += PASS) {
             int st[E], ln[E], tot;
             load_ids(base);
             const int ex = lc_block_scan<LC_D4_THREADS>(entries(base, st, ln), scan_sh, &tot);
-            visit(carry + ex, st, ln);
+            place(carry, ex, tot, min(n_ids - base, PASS), st, ln);
             carry += tot;
         }
-        if (wave == 0 && tail_ln > 0 && n_sel < tile0 + tl && tile0 < n_sel + tail_ln) fill(n_sel, tail_st, tail_ln);
-        const int steps = (tl + STEP - 1) / STEP;
-        for (int k = tl + tid; k < steps * STEP; k += LC_D4_THREADS) ph.row[k] = slab_bytes;
+        for (int k = max(n_sel, tile0) + tid; k < tile0 + tl; k += LC_D4_THREADS) ph.row[k - tile0] = min(tail_st + (k - n_sel), row_max) * a.tok;
+        // Rounds of a step per wavefront; each fetches its rows while the round before is computed, without a branch around the loads (behind one the wait for
+        // a step's rows would be for the next step's too), so that there are rows, past the resource's end, for up to two rounds more.
+        const int rounds = (tl + LC_D4_WAVES * STEP - 1) / (LC_D4_WAVES * STEP);
+        for (int k = tl + tid; k < (rounds + 2) * LC_D4_WAVES * STEP; k += LC_D4_THREADS) ph.row[k] = slab_bytes;
         __syncthreads();
-        // a step's rows are fetched while the one before is computed
         Step x, y;
-        int i = wave;
-        if (i < steps) load(x, i * STEP);
-        for (; i < steps; i += 2 * LC_D4_WAVES) {
-            const int j = i + LC_D4_WAVES, k = i + 2 * LC_D4_WAVES;
-            if (j < steps) load(y, j * STEP);
-            attend(x, i * STEP, tl);
-            if (k < steps) load(x, k * STEP);
-            if (j < steps) attend(y, j * STEP, tl);
+        load(x, wave * STEP);
+        for (int i = 0; i < rounds; i += 2) {
+            const int at = (i * LC_D4_WAVES + wave) * STEP;
+            load(y, at + LC_D4_WAVES * STEP);
+            __builtin_amdgcn_sched_barrier(0);                      // (all of a round's loads are on their way before the round before is waited for)
+            attend(x, at, tl);
+            if (i + 1 >= rounds) break;
+            load(x, at + 2 * LC_D4_WAVES * STEP);
+            __builtin_amdgcn_sched_barrier(0);
+            attend(y, at + LC_D4_WAVES * STEP, tl);
         }
     }
 
@@ -404,7 +429,7 @@ lc_decode4_kernel(const LcDecode4Args a) {
             float den = 0.f;
 #pragma unroll
             for (int w = 0; w < LC_D4_WAVES; ++w) {
-                const float f = exp2f(ph.comb.ml[w][g][0] - ref);
+                const float f = __builtin_amdgcn_exp2f(ph.comb.ml[w][g][0] - ref);
 #pragma unroll
                 for (int t = TERMS - 1; t >= 0; --t) {
                     const float4 x = *reinterpret_cast<const float4*>(&ph.comb.acc[w][WIDE ? 8 * t + g : t * G + g][4 * c4]);
@@ -428,37 +453,52 @@ lc_decode4_kernel(const LcDecode4Args a) {
     const __amdgpu_buffer_rsrc_t pacc_r = lc_buffer(a.part_acc + (size_t)bh * S * G * LC_D, S_eff * G * LC_D * 4);
     const float* pml = a.part_ml + (size_t)bh * S * G * 2;
     constexpr int WAYS = (LC_D4_THREADS / NV) > 0 ? (LC_D4_THREADS / NV) : 1;
-    constexpr int MR = 8;                                    // partials per round and thread
+    constexpr int MR = 16;                                   // partials per round and thread
     const int v = tid % NV, wy = tid / NV;
     const int g = v / (LC_D / 4), c4 = v % (LC_D / 4);
     float4 x[MR];
-    auto load_round = [&](int sp0) LC_INLINE {
+    auto load_round = [&](int sp0) LC_INLINE {               // (past the last split: zeros)
 #pragma unroll
         for (int k = 0; k < MR; ++k) x[k] = lc_load_agent4(pacc_r, (((sp0 + k * WAYS) * G + g) * LC_D + 4 * c4) * 4);
     };
     load_round(wy);
-    for (int i = tid; i < S_eff * G; i += LC_D4_THREADS) {
-        ph.merge.m[i] = lc_load_agent(pml + 2 * i);
-        ph.merge.l[i] = lc_load_agent(pml + 2 * i + 1);
+    // Every 32 lanes have one head (slot v of the output) and turn its splits' references and sums into scales by themselves.
+    const int half = tid >> 5, hl = tid & 31;
+    float m_all = LC_NEG_INF, den = 0.f;
+    for (int sp = hl; sp < S_eff; sp += 32) {
+        const float m = lc_load_agent(pml + 2 * (sp * G + g)), l = lc_load_agent(pml + 2 * (sp * G + g) + 1);
+        ph.merge.scale[half][sp] = m;
+        ph.merge.sum[half][sp] = l;
+        m_all = fmaxf(m_all, m);
     }
-    __syncthreads();
-    float m = LC_NEG_INF;
-    for (int sp = 0; sp < S_eff; ++sp) m = fmaxf(m, ph.merge.m[sp * G + g]);
-    const float ref = m == LC_NEG_INF ? 0.f : m;
-    float den = 0.f;
-    for (int sp = 0; sp < S_eff; ++sp) den = fmaf(ph.merge.l[sp * G + g], exp2f(ph.merge.m[sp * G + g] - ref), den);
+    m_all = fmaxf(m_all, lc_dpp<0xB1>(m_all));
+    m_all = fmaxf(m_all, lc_dpp<0x4E>(m_all));
+    m_all = fmaxf(m_all, lc_dpp<0x141>(m_all));
+    m_all = fmaxf(m_all, lc_dpp<0x140>(m_all));
+    {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(m_all), __float_as_uint(m_all), false, false);
+        m_all = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    const float ref = m_all == LC_NEG_INF ? 0.f : m_all;
+    const int n_slots = (S_eff + MR * WAYS - 1) / (MR * WAYS) * (MR * WAYS);
+    for (int sp = hl; sp < n_slots; sp += 32) {              // (this lane's own entries; up to the end of the last round, where sums are zero)
+        const float f = sp < S_eff ? __builtin_amdgcn_exp2f(ph.merge.scale[half][sp] - ref) : 0.f;
+        if (sp < S_eff) den = fmaf(ph.merge.sum[half][sp], f, den);
+        ph.merge.scale[half][sp] = f;
+    }
+    den = lc_sum16(den);
+    den = lc_add_rows(den, den);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
     float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
     if (wy < WAYS) {
         for (int sp0 = wy; sp0 < S_eff; sp0 += MR * WAYS) {
             if (sp0 != wy) load_round(sp0);
 #pragma unroll
             for (int k = 0; k < MR; ++k) {
-                const int sp = sp0 + k * WAYS;
-                if (sp < S_eff) {
-                    const float f = exp2f(ph.merge.m[sp * G + g] - ref);
-                    num.x = fmaf(x[k].x, f, num.x); num.y = fmaf(x[k].y, f, num.y);
-                    num.z = fmaf(x[k].z, f, num.z); num.w = fmaf(x[k].w, f, num.w);
-                }
+                const float f = ph.merge.scale[half][sp0 + k * WAYS];
+                num.x = fmaf(x[k].x, f, num.x); num.y = fmaf(x[k].y, f, num.y);
+                num.z = fmaf(x[k].z, f, num.z); num.w = fmaf(x[k].w, f, num.w);
             }
         }
     }
