@@ -4,6 +4,8 @@
 #include "lc_internal.h"
 #include "lc_select.h"
 
+#include <type_traits>
+
 #define LC_LOG2E 1.4426950408889634f
 #define LC_INLINE __attribute__((always_inline))
 #define LC_WG_THREADS 256
@@ -144,7 +146,8 @@ int launch_weigh(const LcWeighArgs& a, int G, hipStream_t stream) {
 #define LC_EV_THREADS 1024
 #define LC_EV_DIGIT 11
 #define LC_EV_BINS (1 << LC_EV_DIGIT)
-#define LC_EV_FEW 256             // chunks among which the cut is found by comparing each with each
+#define LC_EV_FEW 64              // chunks among which the cut is found by comparing each with each
+#define LC_EV_FUSED_MAX 4096      // chunks up to which the selecting workgroup sums the weights itself
 
 // Order-preserving map of a double: larger weight, larger key; what is not a number comes last (key 0).
 __device__ __forceinline__ unsigned long long lc_weight_key(double w) {
@@ -152,177 +155,286 @@ __device__ __forceinline__ unsigned long long lc_weight_key(double w) {
     const unsigned long long u = (unsigned long long)__double_as_longlong(w + 0.0);
     return (u >> 63) ? ~u : (u | (1ull << 63));
 }
+// A chunk's weight summed over the heads, in 64 bits: the order of two chunks does not hang on the rounding of their sums.
+__device__ __forceinline__ double lc_chunk_weight(const float* w, int H, int cap) {
+    double sum = 0.0;
+    int h = 0;
+    for (; h + 4 <= H; h += 4) {
+        float x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = w[(size_t)(h + i) * cap];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum += (double)x[i];
+    }
+    for (; h < H; ++h) sum += (double)w[(size_t)h * cap];
+    return sum;
+}
 
-// A sequence's chunks with their weight summed over the heads (in 64 bits, so that the order does not hang on the sum's), as keys.
 __global__ void __launch_bounds__(256)
 lc_evict_keys_kernel(LcDev ix, const float* weights, unsigned long long* keys) {
     const int b = blockIdx.y, M = min(ix.state[b * ix.H * 4 + 1], ix.cap[0]);
-    for (int j = blockIdx.x * 256 + threadIdx.x; j < M; j += gridDim.x * 256) {
-        const float* w = weights + (size_t)b * ix.H * ix.cap[0] + j;
-        double sum = 0.0;
-        for (int h = 0; h < ix.H; ++h) sum += (double)w[(size_t)h * ix.cap[0]];
-        keys[(size_t)b * ix.cap[0] + j] = lc_weight_key(sum);
-    }
+    for (int j = blockIdx.x * 256 + threadIdx.x; j < M; j += gridDim.x * 256)
+        keys[(size_t)b * ix.cap[0] + j] = lc_weight_key(lc_chunk_weight(weights + (size_t)b * ix.H * ix.cap[0] + j, ix.H, ix.cap[0]));
 }
 
 struct LcEvictArgs {
     LcDev ix;
+    const float* weights;
     const unsigned long long* keys;
     int32_t *ids, *bounds, *counts, *lens;
     int keep, recent, sink;
 };
 
-__device__ __forceinline__ unsigned long long lc_shfl_xor64(unsigned long long v, int m) {
-    const uint32_t lo = __shfl_xor((uint32_t)v, m), hi = __shfl_xor((uint32_t)(v >> 32), m);
-    return ((unsigned long long)hi << 32) | lo;
+// Minimum or maximum over the wavefront, in lane 63 (DPP shifts; lanes without a source keep their own).
+template <bool MAX>
+__device__ __forceinline__ uint32_t lc_wave_extreme(uint32_t v) {
+    auto step = [&](uint32_t x) LC_INLINE { v = MAX ? max(v, x) : min(v, x); };
+    step((uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x111, 0xF, 0xF, false));   // row_shr:1
+    step((uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x112, 0xF, 0xF, false));   // row_shr:2
+    step((uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x114, 0xF, 0xF, false));   // row_shr:4
+    step((uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x118, 0xF, 0xF, false));   // row_shr:8
+    step((uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x142, 0xA, 0xF, false));   // row_bcast:15 -> rows 1, 3
+    step((uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x143, 0xC, 0xF, false));   // row_bcast:31 -> rows 2, 3
+    return v;
 }
 
 // One workgroup per sequence: the pinned chunks, and of the others the longest prefix by (key descending, id ascending) that fits.  The cut
-// is found digit by digit from the first bit in which keys differ: tokens per digit, then the digit at which their sum from above no longer fits.
+// is found digit by digit of the keys' distance from the smallest: tokens per digit, then the digit at which their sum from above no longer fits,
+// until few chunks are left at the cut (mostly after one digit) or all their keys are equal.  (Digits of the keys themselves begin with the
+// exponent, whose few values put all LDS atomics on a few words.)
+// A thread keeps C chunks, 1024 apart, in registers; chunks beyond (more than 12288, or an index that has grown since the launch was captured) are read where they are
+// each time.
+// What bounds it is a chain of barriers, LDS atomics and the first loads in one compute unit per sequence.
+template <int C, bool FUSED>
 __global__ void __launch_bounds__(LC_EV_THREADS)
 lc_evict_select_kernel(const LcEvictArgs a) {
     lc_fetch_args<sizeof(LcEvictArgs)>();
     constexpr int NT = LC_EV_THREADS, NW = NT / 64;
-    __shared__ int tok_sh[LC_EV_BINS], cnt_sh[LC_EV_BINS];
-    __shared__ unsigned long long key_sh[LC_EV_FEW], red_sh[2 * NW];
-    __shared__ int id_sh[LC_EV_FEW], len_sh[LC_EV_FEW], keep_sh[LC_EV_FEW];
-    __shared__ int scan_sh[2 * NW], found_sh[4], few_sh;
+    __shared__ int tok_sh[LC_EV_BINS];
+    __shared__ unsigned long long key_sh[LC_EV_FEW], last_key_sh;
+    __shared__ uint32_t red_sh[3 * NW];
+    __shared__ int id_sh[LC_EV_FEW], len_sh[LC_EV_FEW], sum_sh[LC_EV_FEW];
+    __shared__ int scan_sh[2 * NW], found_sh[2], few_sh, last_id_sh;
+    __shared__ int slab_cnt[C * NW], slab_tok[C * NW];
     const LcDev& ix = a.ix;
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int T = ix.state[b * ix.H * 4 + 0], M = min(ix.state[b * ix.H * 4 + 1], ix.cap[0]);
     const int* bnd = ix.bounds + (size_t)b * (ix.cap[0] + 1);
     const unsigned long long* keys = a.keys + (size_t)b * ix.cap[0];
+    const float* weights = a.weights + (size_t)b * ix.H * ix.cap[0];
     const int last = bnd[M];
-    auto pinned = [&](int begin, int end) { return begin < a.sink || end > last - a.recent; };
+    auto key_of = [&](int j) LC_INLINE { return FUSED ? lc_weight_key(lc_chunk_weight(weights + j, ix.H, ix.cap[0])) : keys[j]; };
+    auto pinned = [&](int begin, int end) LC_INLINE { return begin < a.sink || end > last - a.recent; };
 
-    // tokens of the pinned chunks and of the others; the smallest and the largest key of those
-    int pin = 0;
-    unsigned long long lo = ~0ull, hi = 0ull;
-    for (int j = tid; j < M; j += NT) {
-        const int begin = bnd[j], end = bnd[j + 1];
-        if (pinned(begin, end)) {
-            pin += end - begin;
-        } else {
-            const unsigned long long k = keys[j];
-            lo = min(lo, k);
-            hi = max(hi, k);
-        }
-    }
-    int pin_all;
-    lc_block_scan<NT>(pin, scan_sh, &pin_all);
+    unsigned long long key[C];
+    int len[C];
+    uint32_t pins = 0u, live = 0u;                           // bit c: this thread's chunk c is pinned, may be kept or not
+    {
+        int end[C];
+        // (no branch around a load: they are on their way together)
 #pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-        lo = min(lo, lc_shfl_xor64(lo, m));
-        hi = max(hi, lc_shfl_xor64(hi, m));
-    }
-    if (lane == 0) { red_sh[wave] = lo; red_sh[NW + wave] = hi; }
-    __syncthreads();
-    for (int w = 0; w < NW; ++w) {
-        lo = min(lo, red_sh[w]);
-        hi = max(hi, red_sh[NW + w]);
-    }
-    int left = max(0, a.keep - pin_all);                     // tokens for the others
-
-    // Keys above `above` are kept, those below are not; of those with the bits of `cut` above `shift` the first `left` tokens' worth.
-    unsigned long long cut = 0ull;
-    int shift = 64;                                          // (64: every key)
-    bool all = last - pin_all <= left;
-    int few = -1;                                            // chunks around the cut in the lists, if there are not many
-    if (!all && lo < hi) shift = 64 - __clzll((long long)(lo ^ hi));
-    if (!all) cut = shift == 64 ? 0ull : lo >> shift;
-    auto inside = [&](unsigned long long k) { return shift == 64 || (k >> shift) == cut; };
-    if (!all && lo == hi) { shift = 0; cut = lo; }
-    while (!all && shift > 0 && few < 0) {
-        const int next = max(0, shift - LC_EV_DIGIT), digits = 1 << (shift - next);
-        for (int i = tid; i < LC_EV_BINS; i += NT) tok_sh[i] = cnt_sh[i] = 0;
-        __syncthreads();
-        for (int j = tid; j < M; j += NT) {
-            const int begin = bnd[j], end = bnd[j + 1];
-            const unsigned long long k = keys[j];
-            if (!pinned(begin, end) && inside(k)) {
-                const int d = (int)((k >> next) & (unsigned long long)(digits - 1));
-                atomicAdd(&tok_sh[d], end - begin);
-                atomicAdd(&cnt_sh[d], 1);
-            }
+        for (int c = 0; c < C; ++c) {
+            const int j = max(0, min(tid + c * NT, M - 1));
+            len[c] = bnd[j];
+            end[c] = bnd[j + 1];
+            key[c] = key_of(j);
         }
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const uint32_t real = tid + c * NT < M ? 1u : 0u, pin = pinned(len[c], end[c]) ? 1u : 0u;
+            pins |= (real & pin) << c;
+            live |= (real & ~pin) << c;
+            len[c] = end[c] - len[c];
+        }
+    }
+    // f(whether it may be kept or not, chunk, its tokens, its key) of the chunks in registers, then of the others
+    auto each = [&](auto f) LC_INLINE {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+            if (c * NT < M) f((live >> c) & 1u, tid + c * NT, len[c], key[c]);
+        for (int j = C * NT + tid; j < M; j += NT) {
+            const int begin = bnd[j], end = bnd[j + 1];
+            if (!pinned(begin, end)) f(1u, j, end - begin, key_of(j));
+        }
+    };
+
+    // tokens of those, the smallest and the largest of their keys (of the upper halves)
+    int tok = 0;
+    uint32_t lo = 0xffffffffu, hi = 0u;
+    each([&](uint32_t is, int, int n, unsigned long long k) LC_INLINE {
+        const uint32_t none = is - 1u, top = (uint32_t)(k >> 32);    // (all ones where it is not)
+        tok += n & ~(int)none;
+        lo = min(lo, top | none);
+        hi = max(hi, top & ~none);
+    });
+    for (int i = tid; i < LC_EV_BINS; i += NT) tok_sh[i] = 0;
+    if (tid < LC_EV_FEW) sum_sh[tid] = 0;
+    if (tid == 0) { few_sh = 0; last_key_sh = 0ull; last_id_sh = -1; }
+    lo = lc_wave_extreme<false>(lo);
+    hi = lc_wave_extreme<true>(hi);
+    tok = lc_wave_scan_incl(tok);
+    if (lane == 63) { red_sh[wave] = lo; red_sh[NW + wave] = hi; red_sh[2 * NW + wave] = (uint32_t)tok; }
+    __syncthreads();
+    lo = (uint32_t)lc_readlane((int)lc_wave_extreme<false>(red_sh[lane & (NW - 1)]), 63);
+    hi = (uint32_t)lc_readlane((int)lc_wave_extreme<true>(red_sh[NW + (lane & (NW - 1))]), 63);
+    const int others = lc_readlane(lc_wave_scan_incl(lane < NW ? (int)red_sh[2 * NW + lane] : 0), 63);
+    int left = max(0, a.keep - (last - others));             // tokens for the others, behind the pinned ones
+
+    // Keys of [base, base + 2^shift) are at the cut: of those the first `left` tokens' worth is kept, of larger ones all, of smaller ones none.
+    const bool all = others <= left;
+    unsigned long long base = (unsigned long long)lo << 32;
+    int shift = 32 + (lo < hi ? 32 - __clz((int)(hi - lo)) : 0);
+    auto at_cut = [&](unsigned long long k) LC_INLINE { return shift == 64 ? true : ((k - base) >> shift) == 0ull; };
+    bool few = false;
+    while (!all && shift > 0 && !few) {
+        const int next = max(0, shift - LC_EV_DIGIT);
+        each([&](uint32_t is, int, int n, unsigned long long k) LC_INLINE {
+            if (is && at_cut(k)) atomicAdd(&tok_sh[(int)((k - base) >> next)], n);
+        });
         __syncthreads();
         // from the largest digit down: thread t has digits (BINS - 1 - 2 t) and the one below
         const int d1 = LC_EV_BINS - 1 - 2 * tid, t1 = tok_sh[d1], t0 = tok_sh[d1 - 1];
         int total;
         const int before = lc_block_scan<NT>(t1 + t0, scan_sh, &total);
-        if (before <= left && before + t1 > left) { found_sh[0] = d1; found_sh[1] = before; found_sh[2] = cnt_sh[d1]; }
-        else if (before + t1 <= left && before + t1 + t0 > left) { found_sh[0] = d1 - 1; found_sh[1] = before + t1; found_sh[2] = cnt_sh[d1 - 1]; }
+        if (before <= left && before + t1 > left) { found_sh[0] = d1; found_sh[1] = before; }
+        else if (before + t1 <= left && before + t1 + t0 > left) { found_sh[0] = d1 - 1; found_sh[1] = before + t1; }
+        tok_sh[d1] = tok_sh[d1 - 1] = 0;
         __syncthreads();
-        cut = (shift == 64 ? 0ull : cut << (shift - next)) | (unsigned long long)found_sh[0];
+        base += (unsigned long long)found_sh[0] << next;
         left -= found_sh[1];
         shift = next;
-        if (found_sh[2] <= LC_EV_FEW) few = found_sh[2];
-        __syncthreads();
-    }
-    if (few >= 0) {
-        // the chunks at the cut, compared with each other
-        if (tid == 0) few_sh = 0;
-        __syncthreads();
-        for (int j = tid; j < M; j += NT) {
-            const int begin = bnd[j], end = bnd[j + 1];
-            const unsigned long long k = keys[j];
-            if (!pinned(begin, end) && inside(k)) {
+        // the chunks at the cut, if they are few
+        each([&](uint32_t is, int j, int n, unsigned long long k) LC_INLINE {
+            if (is && at_cut(k)) {
                 const int i = atomicAdd(&few_sh, 1);
-                key_sh[i] = k;
-                id_sh[i] = j;
-                len_sh[i] = end - begin;
+                if (i < LC_EV_FEW) {
+                    key_sh[i] = k;
+                    id_sh[i] = j;
+                    len_sh[i] = n;
+                }
+            }
+        });
+        __syncthreads();
+        few = few_sh <= LC_EV_FEW;
+        if (!few) {
+            __syncthreads();
+            if (tid == 0) few_sh = 0;
+            __syncthreads();
+        }
+    }
+    // Every chunk up to (last_key, last_id) in the order is kept.
+    if (few) {
+        // a lane has a chunk at the cut, each wavefront some of those to compare it with
+        const int n = few_sh;
+        const unsigned long long k = lane < n ? key_sh[lane] : 0ull;
+        const int id = lane < n ? id_sh[lane] : 0x7fffffff;
+        int part = 0;
+        for (int i = wave; i < n; i += NW) {
+            const unsigned long long ki = key_sh[i];
+            if (ki > k || (ki == k && id_sh[i] <= id)) part += len_sh[i];
+        }
+        if (lane < n && part != 0) atomicAdd(&sum_sh[lane], part);
+        __syncthreads();
+        if (wave == 0) {
+            // (the sums of those that fit grow along the order: the last of them has the largest)
+            const int sum = sum_sh[lane];
+            const uint32_t mine = lane < n && sum <= left ? (uint32_t)sum + 1u : 0u;
+            const uint32_t most = (uint32_t)lc_readlane((int)lc_wave_extreme<true>(mine), 63);
+            if (most == 0u) {
+                if (lane == 0) last_key_sh = base + ((1ull << shift) - 1ull);    // none at the cut
+            } else if (mine == most) {
+                last_key_sh = k;
+                last_id_sh = id;
             }
         }
-        __syncthreads();
-        if (tid < few) {
-            const unsigned long long k = key_sh[tid];
-            const int id = id_sh[tid];
-            int sum = len_sh[tid];
-            for (int i = 0; i < few; ++i)
-                if (key_sh[i] > k || (key_sh[i] == k && id_sh[i] < id)) sum += len_sh[i];
-            keep_sh[tid] = sum <= left;
-        }
-        __syncthreads();
     }
+    if (!all && !few) {
+        // equal keys at the cut: the first of them
+        int tied = 0;
+        for (int j0 = 0; j0 < M; j0 += NT) {
+            const int j = j0 + tid;
+            int n = 0;
+            if (j < M) {
+                const int begin = bnd[j], end = bnd[j + 1];
+                if (!pinned(begin, end) && key_of(j) == base) n = end - begin;
+            }
+            int total;
+            const int before = lc_block_scan<NT>(n, scan_sh, &total);
+            if (n > 0 && before <= left - tied - n) atomicMax(&last_id_sh, j);
+            tied = min(tied + total, 1 << 30);
+        }
+        if (tid == 0) last_key_sh = base;
+    }
+    __syncthreads();
+    const unsigned long long last_key = all ? 0ull : last_key_sh;
+    const int last_id = all ? 0x7fffffff : last_id_sh;
+    auto keeps = [&](unsigned long long k, int j) LC_INLINE { return k > last_key || (k == last_key && j <= last_id); };
 
     // ids, boundaries, the rest of both lists
     int32_t* ids = a.ids + (size_t)b * ix.cap[0];
     int32_t* bounds = a.bounds + (size_t)b * (ix.cap[0] + 1);
-    int n_keep = 0, n_tok = 0, tied = 0;                     // so far; tokens at the cut, where all keys there are equal
-    for (int j0 = 0; j0 < M; j0 += NT) {
-        const int j = j0 + tid;
-        bool keep = false, tie = false;
-        int len = 0;
-        if (j < M) {
-            const int begin = bnd[j], end = bnd[j + 1];
-            len = end - begin;
-            keep = all || pinned(begin, end);
-            if (!keep) {
-                const unsigned long long k = keys[j];
-                if (!inside(k)) {
-                    keep = (k >> shift) > cut;
-                } else if (few >= 0) {
-                    for (int i = 0; i < few; ++i)
-                        if (id_sh[i] == j) keep = keep_sh[i] != 0;
-                } else {
-                    tie = true;
+    int n_keep = 0, n_tok = 0;
+    {
+        // the chunks in registers all at once: wavefronts' counts and tokens, then each its place
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int j = tid + c * NT;
+            int count = 0, tokens = 0;
+            if (c * NT < M) {
+                const bool k = ((pins | (keeps(key[c], j) ? live : 0u)) >> c) & 1u;
+                pins = k ? pins | (1u << c) : pins;          // (from here on: kept)
+                const int n = k ? len[c] : 0;
+                tokens = lc_wave_scan_incl(n);
+                len[c] = tokens - n;                         // (from here on: tokens kept before it, of the wavefront)
+                count = __popcll(__ballot(k));
+            }
+            if (lane == 63) { slab_cnt[c * NW + wave] = count; slab_tok[c * NW + wave] = tokens; }
+        }
+        __syncthreads();
+        if (wave == 0) {
+            int cc = 0, tt = 0;
+#pragma unroll
+            for (int i = 0; i < (C * NW + 63) / 64; ++i) {
+                const int x = i * 64 + lane;
+                const int c = x < C * NW ? slab_cnt[x] : 0, t = x < C * NW ? slab_tok[x] : 0;
+                const int ci = lc_wave_scan_incl(c), ti = lc_wave_scan_incl(t);
+                if (x < C * NW) { slab_cnt[x] = cc + ci - c; slab_tok[x] = tt + ti - t; }
+                cc += lc_readlane(ci, 63);
+                tt += lc_readlane(ti, 63);
+            }
+            if (lane == 0) { found_sh[0] = cc; found_sh[1] = tt; }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+            if (c * NT < M) {
+                const bool k = (pins >> c) & 1u;
+                const int i = slab_cnt[c * NW + wave] + __popcll(__ballot(k) & ((1ull << lane) - 1ull));
+                if (k) {
+                    ids[i] = tid + c * NT;
+                    bounds[i] = slab_tok[c * NW + wave] + len[c];
                 }
             }
+        n_keep = found_sh[0];
+        n_tok = found_sh[1];
+    }
+    for (int j0 = C * NT; j0 < M; j0 += NT) {
+        const int j = j0 + tid;
+        bool keep = false;
+        int n = 0;
+        if (j < M) {
+            const int begin = bnd[j], end = bnd[j + 1];
+            n = end - begin;
+            keep = all || pinned(begin, end) || keeps(key_of(j), j);
         }
-        if (few < 0 && !all) {
-            int total;
-            const int before = lc_block_scan<NT>(tie ? len : 0, scan_sh, &total);
-            if (tie) keep = tied + before + len <= left;
-            tied = min(tied + total, 1 << 30);
-        }
-        int at, tok, n, t;
-        lc_block_scan2<NT>(keep ? 1 : 0, keep ? len : 0, scan_sh, &at, &tok, &n, &t);
+        int at, to, count, tokens;
+        lc_block_scan2<NT>(keep ? 1 : 0, keep ? n : 0, scan_sh, &at, &to, &count, &tokens);
         if (keep) {
             ids[n_keep + at] = j;
-            bounds[n_keep + at] = n_tok + tok;
+            bounds[n_keep + at] = n_tok + to;
         }
-        n_keep += n;
-        n_tok += t;
+        n_keep += count;
+        n_tok += tokens;
     }
     for (int i = n_keep + tid; i < ix.cap[0]; i += NT) {
         ids[i] = -1;
@@ -337,7 +449,8 @@ lc_evict_select_kernel(const LcEvictArgs a) {
 
 // ---------------------------------------------------------------- the rows that stay
 #define LC_ER_THREADS 256
-#define LC_ER_ROWS 64             // new rows of a workgroup
+#define LC_ER_ROWS 64             // new rows of a tile
+#define LC_ER_GROUPS 4096         // workgroups for rows at most; each goes on to further tiles
 
 struct LcEvictRowsArgs {
     LcDev ix;
@@ -351,13 +464,19 @@ struct LcEvictRowsArgs {
     int row_tiles;        // workgroups that move rows; those behind move weights
 };
 
-// New rows [64 x, 64 x + 64) of a (sequence, head), keys and values: the rows of the kept chunks one behind the other, then the open tail's.
-template <int BYTES>      // of a row
+// The piece of a 4-bit row that a lane moves at a time: rows are 4-byte aligned.
+typedef int LcPiece4 __attribute__((ext_vector_type(4), aligned(4)));
+
+// A tile is ROWS new rows of a (sequence, head), keys and values: the rows of the kept chunks one behind the other, then the open tail's.  Bound by the
+// bytes where chunks are long (16 K of 32 K tokens of 4 sequences, 8 heads, bfloat16: 538 MB in 114 us); chunks of a dozen tokens in 4 bits are runs of 0.8 KB,
+// which the memory reads at 3.1 TB/s of useful bytes.  Before those a tile has a chain of five loads to find its rows.  (Tiles of 128 and 256 rows in 4
+// bits: 24.6 and 28.3 us where 64 take 23.0; several heads to a workgroup, which share the rows' places: 23.9 to 26.6, bfloat16 116.)
+template <int BYTES, int ROWS>    // bytes of a row
 __global__ void __launch_bounds__(LC_ER_THREADS)
 lc_evict_rows_kernel(const LcEvictRowsArgs a) {
     lc_fetch_args<sizeof(LcEvictRowsArgs)>();
-    __shared__ int bound_sh[LC_ER_ROWS + 1];
-    __shared__ int row_sh[LC_ER_ROWS];
+    __shared__ int bound_sh[ROWS], begin_sh[ROWS];
+    __shared__ int row_sh[ROWS];
     const LcDev& ix = a.ix;
     const int h = blockIdx.y, b = blockIdx.z, bh = b * ix.H + h, tid = threadIdx.x, lane = tid & 63;
     const int cap = ix.cap[0];
@@ -374,10 +493,10 @@ lc_evict_rows_kernel(const LcEvictRowsArgs a) {
         return;
     }
     const int last = bnd[M], n_kept = max(0, min(kept[n], T)), rows = min(n_kept + max(0, T - last), a.max_tokens);
-    // (the grid is laid out for the host's count of tokens; a captured graph may find more)
-    for (int r0 = blockIdx.x * LC_ER_ROWS; r0 < rows; r0 += a.row_tiles * LC_ER_ROWS) {
+    const size_t from = (size_t)b * a.seq + (size_t)h * a.head, to = (size_t)b * a.seq_to + (size_t)h * a.head_to;
+    for (int r0 = blockIdx.x * ROWS; r0 < rows; r0 += a.row_tiles * ROWS) {
         // the last kept chunk that begins at or before r0: 64 boundaries at a time, each round a 64th of the range
-        int lo = 0, len = n;                                     // boundaries lo .. lo + len - 1 are candidates, kept[lo] <= r0
+        int lo = 0, len = n;                                 // boundaries lo .. lo + len - 1 are candidates, kept[lo] <= r0
         while (len > 1) {
             const int step = (len + 63) / 64;
             const int i = lane * step;
@@ -387,33 +506,61 @@ lc_evict_rows_kernel(const LcEvictRowsArgs a) {
             lo += at;
             len = min(step, len - at);
         }
-        // a row lies in one of the next 64 chunks, or behind them all in the tail
-        if (tid <= LC_ER_ROWS) bound_sh[tid] = lo + tid < n ? kept[lo + tid] : 0x7fffffff;
+        // a row lies in one of the next ROWS chunks, or behind them all in the tail
+        if (tid < ROWS) {
+            const bool real = lo + tid < n;
+            const int at = real ? kept[lo + tid] : 0x7fffffff, id = real ? ids[lo + tid] : 0;
+            bound_sh[tid] = at;
+            begin_sh[tid] = bnd[max(0, min(id, M - 1))];
+        }
         __syncthreads();
-        if (tid < LC_ER_ROWS) {
+        if (tid < ROWS) {
             const int r = r0 + tid;
             int row = last + (r - n_kept);
             if (r < n_kept) {
                 int i = 0;
-    #pragma unroll
-                for (int s = 32; s > 0; s >>= 1)
+#pragma unroll
+                for (int s = ROWS / 2; s > 0; s >>= 1)
                     if (bound_sh[i + s] <= r) i += s;
-                const int id = max(0, min(ids[lo + i], M - 1));
-                row = bnd[id] + (r - bound_sh[i]);
+                row = begin_sh[i] + (r - bound_sh[i]);
             }
             row_sh[tid] = max(0, min(row, T - 1));
         }
         __syncthreads();
-        const int m = min(LC_ER_ROWS, rows - r0);
-        using Piece = typename std::conditional<BYTES % 16 == 0, uint4, uint32_t>::type;
-        constexpr int PIECES = BYTES / (int)sizeof(Piece);
-        const size_t from = (size_t)b * a.seq + (size_t)h * a.head, to = (size_t)b * a.seq_to + (size_t)h * a.head_to;
-        for (int i = tid; i < m * PIECES; i += LC_ER_THREADS) {
-            const int r = i / PIECES, c = i % PIECES;
-            const size_t f = from + (size_t)row_sh[r] * a.tok + c * sizeof(Piece), t = to + (size_t)(r0 + r) * a.tok_to + c * sizeof(Piece);
-            const Piece k = *reinterpret_cast<const Piece*>(a.K + f), v = *reinterpret_cast<const Piece*>(a.V + f);
-            *reinterpret_cast<Piece*>(a.K_to + t) = k;
-            *reinterpret_cast<Piece*>(a.V_to + t) = v;
+        const int m = min(ROWS, rows - r0);
+        // (all of a thread's loads before its stores)
+        using Piece = typename std::conditional<BYTES % 16 == 0, lc_v4i, LcPiece4>::type;
+        constexpr int PIECES = BYTES / 16, PER = ROWS * PIECES / LC_ER_THREADS;
+        static_assert(BYTES - 16 * PIECES == 0 || (BYTES - 16 * PIECES == 4 && ROWS <= LC_ER_THREADS), "");
+        lc_v4i k[PER], v[PER];
+        uint32_t ks = 0u, vs = 0u;
+#pragma unroll
+        for (int u = 0; u < PER; ++u) {
+            const int i = tid + u * LC_ER_THREADS, r = i / PIECES;
+            if (r < m) {
+                const size_t f = from + (size_t)row_sh[r] * a.tok + i % PIECES * 16;
+                k[u] = *reinterpret_cast<const Piece*>(a.K + f);
+                v[u] = *reinterpret_cast<const Piece*>(a.V + f);
+            }
+        }
+        if (BYTES % 16 != 0 && tid < m) {
+            const size_t f = from + (size_t)row_sh[tid] * a.tok + 16 * PIECES;
+            ks = *reinterpret_cast<const uint32_t*>(a.K + f);
+            vs = *reinterpret_cast<const uint32_t*>(a.V + f);
+        }
+#pragma unroll
+        for (int u = 0; u < PER; ++u) {
+            const int i = tid + u * LC_ER_THREADS, r = i / PIECES;
+            if (r < m) {
+                const size_t t = to + (size_t)(r0 + r) * a.tok_to + i % PIECES * 16;
+                *reinterpret_cast<Piece*>(a.K_to + t) = k[u];
+                *reinterpret_cast<Piece*>(a.V_to + t) = v[u];
+            }
+        }
+        if (BYTES % 16 != 0 && tid < m) {
+            const size_t t = to + (size_t)(r0 + tid) * a.tok_to + 16 * PIECES;
+            *reinterpret_cast<uint32_t*>(a.K_to + t) = ks;
+            *reinterpret_cast<uint32_t*>(a.V_to + t) = vs;
         }
         __syncthreads();                                     // (the lists have been used)
     }
@@ -476,12 +623,13 @@ int evict_rows(const lc_index* idx, const int32_t* keep_ids, const int32_t* keep
     int most = 0;
     for (int b = 0; b < idx->B; ++b)
         if (idx->T[b] > most) most = idx->T[b];
-    a.row_tiles = most > 0 ? (most + LC_ER_ROWS - 1) / LC_ER_ROWS : 1;
+    const int tiles = most > LC_ER_ROWS ? (most + LC_ER_ROWS - 1) / LC_ER_ROWS : 1, fit = (LC_ER_GROUPS + idx->B * idx->H_kv - 1) / (idx->B * idx->H_kv);
+    a.row_tiles = tiles < fit ? tiles : fit;
     const int weight_tiles = weights ? (idx->cfg.max_chunks + LC_ER_THREADS - 1) / LC_ER_THREADS : 0;
     const dim3 grid(a.row_tiles + weight_tiles, idx->H_kv, idx->B);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (in4) hipLaunchKernelGGL(lc_evict_rows_kernel<LC_ROW4>, grid, dim3(LC_ER_THREADS), 0, st, a);
-    else hipLaunchKernelGGL(lc_evict_rows_kernel<2 * LC_D>, grid, dim3(LC_ER_THREADS), 0, st, a);
+    if (in4) hipLaunchKernelGGL((lc_evict_rows_kernel<LC_ROW4, LC_ER_ROWS>), grid, dim3(LC_ER_THREADS), 0, st, a);
+    else hipLaunchKernelGGL((lc_evict_rows_kernel<2 * LC_D, LC_ER_ROWS>), grid, dim3(LC_ER_THREADS), 0, st, a);
     LC_HIP_CHECK(hipGetLastError());
     return LC_OK;
 }
@@ -511,14 +659,21 @@ int lc_evict_select(const lc_index* idx, const float* weights, int keep_tokens, 
     int most = 0;
     for (int b = 0; b < idx->B; ++b)
         if (idx->M[b] > most) most = idx->M[b];
-    hipLaunchKernelGGL(lc_evict_keys_kernel, dim3(most > 0 ? (most + 255) / 256 : 1, idx->B), dim3(256), 0, st, idx->dev, weights, keys);
-    LC_HIP_CHECK(hipGetLastError());
     LcEvictArgs a;
     a.ix = idx->dev;
+    a.weights = weights;
     a.keys = keys;
     a.ids = keep_ids; a.bounds = keep_bounds; a.counts = keep_counts; a.lens = keep_lens;
     a.keep = keep_tokens; a.recent = recent_tokens; a.sink = idx->cfg.sink_tokens;
-    hipLaunchKernelGGL(lc_evict_select_kernel, dim3(idx->B), dim3(LC_EV_THREADS), 0, st, a);
+    const dim3 grid(idx->B), block(LC_EV_THREADS);
+    if (most <= LC_EV_FUSED_MAX) {
+        if (most <= LC_EV_THREADS) hipLaunchKernelGGL((lc_evict_select_kernel<1, true>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((lc_evict_select_kernel<4, true>), grid, block, 0, st, a);
+    } else {
+        hipLaunchKernelGGL(lc_evict_keys_kernel, dim3((most + 255) / 256, idx->B), dim3(256), 0, st, idx->dev, weights, keys);
+        LC_HIP_CHECK(hipGetLastError());
+        hipLaunchKernelGGL((lc_evict_select_kernel<12, false>), grid, block, 0, st, a);
+    }
     LC_HIP_CHECK(hipGetLastError());
     return LC_OK;
 }
