@@ -10,7 +10,9 @@
 #define LC_INLINE __attribute__((always_inline))
 #define LC_WG_THREADS 256
 #define LC_WG_WAVES (LC_WG_THREADS / 64)
-#define LC_WG_LONG 256            // tokens from which on a chunk is shared by the workgroup's wavefronts
+#define LC_WG_LONG 512            // tokens from which on a chunk is shared by the workgroup's wavefronts
+#define LC_WG_ROWS 32             // tokens of a step
+#define LC_WG_WAVES_FULL 8192     // wavefronts up to which each has one chunk
 
 namespace {
 
@@ -30,21 +32,29 @@ struct LcWeighArgs {
     int cap;
     const float* lse;     // [B][H*G]
     float* weights;       // [B][H][cap0]
+    int G;                // heads of a group
+    int per;              // list entries of a workgroup, at most 64
 };
 
-template <int G, bool IN4>
+//
+// A workgroup has `per` (up to 64) entries of a list, whose chunks, boundaries and weights so far come in one go, a lane to an entry; a wavefront takes every fourth of them
+// and goes through their tokens 32 at a time, the next step's keys on their way, the next chunk's behind a chunk's last.
+template <bool IN4>
 __global__ void __launch_bounds__(LC_WG_THREADS)
 lc_weigh_kernel(const LcWeighArgs a) {
     lc_fetch_args<sizeof(LcWeighArgs)>();
     __shared__ float part_sh[LC_WG_WAVES];
     const LcDev& ix = a.ix;
     const int h = blockIdx.y, b = blockIdx.z, bh = b * ix.H + h;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, kg = lane >> 4;
-    const int head = min(n, G - 1);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, kg = lane >> 4;
+    const int G = a.G, head = min(n, G - 1);
+    const int e0 = (int)blockIdx.x * a.per;
+    // this lane's entry, and the one before
+    const __amdgpu_buffer_rsrc_t ids_r = lc_buffer(a.ids + (size_t)bh * a.cap, (int)(min((long long)a.cap, 1LL << 28) * 4));
+    const int id = lc_buf_load_i32(ids_r, e0 + lane), before = e0 + lane > 0 ? lc_buf_load_i32(ids_r, e0 + lane - 1) : -1;
     const int count = max(0, min(a.counts[bh], a.cap)), M = ix.state[bh * 4 + 1];
-    if ((int)blockIdx.x * LC_WG_WAVES >= count) return;
-    const int32_t* ids = a.ids + (size_t)bh * a.cap;
-    const int* bnd = ix.bounds + (size_t)b * (ix.cap[0] + 1);
+    const int n_e = min(a.per, count - e0);
+    if (n_e <= 0) return;
     // the query block as in the attention (bfloat16 rows: lane (kg, n) has columns 8 kg + 32 j, 4-bit rows: 32 kg + 8 j)
     uint4 qb[4];
     {
@@ -52,92 +62,137 @@ lc_weigh_kernel(const LcWeighArgs a) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) qb[j] = *reinterpret_cast<const uint4*>(qh + (IN4 ? 32 * kg + 8 * j : 8 * kg + 32 * j));
     }
-    const float scale = 0.08838834764831845f * LC_LOG2E;
     const float lse = a.lse[(size_t)bh * G + head];
+    float* weights = a.weights + (size_t)bh * ix.cap[0];
+    // (an entry that is no chunk, or no larger than the one before it, is passed over: it has no tokens)
+    const bool real = lane < n_e && id >= 0 && id < M && id > before;
+    const int* bnd = ix.bounds + (size_t)b * (ix.cap[0] + 1);
+    const int at = real ? id : 0;
+    const int begin = bnd[at], end = real ? min(bnd[at + 1], a.max_tokens) : begin;
+    const float so_far = weights[at];
+    const int begin_short = end - begin < LC_WG_LONG ? begin : end;      // long chunks are done behind the others
+
+    const float scale = 0.08838834764831845f * LC_LOG2E;
     const float off = lse == LC_NEG_INF ? LC_NEG_INF : -lse * LC_LOG2E;      // (a head that attended to nothing adds nothing)
-    constexpr int ROW = IN4 ? LC_ROW4 : 2 * LC_D;
+    constexpr int ROW = IN4 ? LC_ROW4 : 2 * LC_D, HALVES = LC_WG_ROWS / 16, PIECES = IN4 ? 1 : 4;
     const int slab_bytes = (a.max_tokens - 1) * a.tok + ROW;
     const __amdgpu_buffer_rsrc_t Kr = lc_buffer(static_cast<const char*>(a.K) + (size_t)b * a.seq + (size_t)h * a.head, slab_bytes);
 
-    struct Keys { lc_v4i k[IN4 ? 1 : 4]; int s; };
-    // rows r .. r + 15 (past `end`: zeros)
-    auto load = [&](Keys& w, int r, int end) LC_INLINE {
-        const int o = r + n < end ? (r + n) * a.tok + 16 * kg : slab_bytes;
+    struct Keys { lc_v4i k[HALVES][PIECES]; int s[HALVES]; };
+    // rows r .. r + 31 (from `hi` on: zeros)
+    auto load = [&](Keys& w, int r, int hi) LC_INLINE {
 #pragma unroll
-        for (int j = 0; j < (IN4 ? 1 : 4); ++j) w.k[j] = __builtin_amdgcn_raw_buffer_load_b128(Kr, o, 64 * j, 0);
-        w.s = IN4 ? lc_buf_load_u8(Kr, o + 64 - 15 * kg) : 0;
-    };
-    auto shares = [&](const Keys& w, int r, int end) LC_INLINE -> float {
-        lc_f32x4 d = {0.f, 0.f, 0.f, 0.f};
+        for (int t = 0; t < HALVES; ++t) {
+            const int row = r + 16 * t + n, o = row < hi ? row * a.tok + 16 * kg : slab_bytes;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            lc_bf16x8 k;
-            if constexpr (IN4) k = __builtin_bit_cast(lc_bf16x8, lc_unpack4((uint32_t)w.k[0][j], lc_scale4((uint32_t)w.s)));
-            else k = __builtin_bit_cast(lc_bf16x8, w.k[j]);
-            d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, __builtin_bit_cast(lc_bf16x8, qb[j]), d, 0, 0, 0);
+            for (int j = 0; j < PIECES; ++j) w.k[t][j] = __builtin_amdgcn_raw_buffer_load_b128(Kr, o, 64 * j, 0);
+            w.s[t] = IN4 ? lc_buf_load_u8(Kr, o + 64 - 15 * kg) : 0;
         }
+    };
+    auto shares = [&](const Keys& w, int r, int hi) LC_INLINE -> float {
         float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum += r + 4 * kg + i < end ? exp2f(fmaf(d[i], scale, off)) : 0.f;
+        for (int t = 0; t < HALVES; ++t) {
+            if (t > 0 && r + 16 * t >= hi) break;            // (the same for the wavefront)
+            lc_f32x4 d = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                lc_bf16x8 k;
+                if constexpr (IN4) k = __builtin_bit_cast(lc_bf16x8, lc_unpack4((uint32_t)w.k[t][0][j], lc_scale4((uint32_t)w.s[t])));
+                else k = __builtin_bit_cast(lc_bf16x8, w.k[t][j]);
+                d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, __builtin_bit_cast(lc_bf16x8, qb[j]), d, 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum += r + 16 * t + 4 * kg + i < hi ? __builtin_amdgcn_exp2f(fmaf(d[i], scale, off)) : 0.f;
+        }
         return sum;
     };
-    // this wavefront's part of a chunk: 16 rows of every `step`
-    auto chunk = [&](int lo, int hi, int r0, int step) LC_INLINE -> float {
-        float sum = 0.f;
-        Keys x, y;
-        load(x, r0, hi);
-        for (int r = r0; r < hi; r += 2 * step) {
-            load(y, r + step, hi);
-            sum += shares(x, r, hi);
-            load(x, r + 2 * step, hi);
-            sum += shares(y, r + step, hi);
-        }
-        return lc_sum64(n < G ? sum : 0.f);
+    auto total = [&](float sum) LC_INLINE -> float {
+        sum = lc_sum16(n < G ? sum : 0.f);
+        sum = lc_add_halves(sum, sum);
+        return lc_add_rows(sum, sum);
     };
-    for (int e0 = blockIdx.x * LC_WG_WAVES; e0 < count; e0 += gridDim.x * LC_WG_WAVES) {
-        // (an entry that is no chunk, or no larger than the one before it, is passed over)
-        auto entry = [&](int e, int* lo, int* hi) LC_INLINE -> int {
-            const int id = ids[e], before = e > 0 ? ids[e - 1] : -1;
-            const bool real = id >= 0 && id < M && id > before;
-            *lo = real ? bnd[id] : 0;
-            *hi = real ? min(bnd[id + 1], a.max_tokens) : 0;
-            return id;
-        };
-        int lo = 0, hi = 0, id = 0;
-        if (e0 + wave < count) id = entry(e0 + wave, &lo, &hi);
-        if (hi > lo && hi - lo < LC_WG_LONG) {
-            const float sum = chunk(lo, hi, lo, 16);
-            if (lane == 0) a.weights[(size_t)bh * ix.cap[0] + id] += sum;
+
+    // the wavefront's steps: entry, first row, the chunk's end
+    struct Place { int e, r, hi; };
+    auto settle = [&](Place& p) LC_INLINE {                    // from the beginning of an entry to one with tokens
+        for (; p.e < n_e; p.e += LC_WG_WAVES) {
+            p.r = lc_readlane(begin_short, p.e);
+            p.hi = lc_readlane(end, p.e);
+            if (p.r < p.hi) return;
         }
-        for (int w = 0; w < LC_WG_WAVES && e0 + w < count; ++w) {
-            id = entry(e0 + w, &lo, &hi);
-            if (hi - lo < LC_WG_LONG) continue;                  // (the same for the workgroup)
-            const float sum = chunk(lo, hi, lo + 16 * wave, 16 * LC_WG_WAVES);
-            if (lane == 0) part_sh[wave] = sum;
-            __syncthreads();
-            if (tid == 0) a.weights[(size_t)bh * ix.cap[0] + id] += (part_sh[0] + part_sh[1]) + (part_sh[2] + part_sh[3]);
-            __syncthreads();
+        p.r = p.hi = 0;
+    };
+    auto next = [&](const Place& p) LC_INLINE -> Place {
+        Place q = {p.e, p.r + LC_WG_ROWS, p.hi};
+        if (q.r >= q.hi) {
+            q.e += LC_WG_WAVES;
+            settle(q);
         }
+        return q;
+    };
+    Place p = {wave, 0, 0};
+    settle(p);
+    float sum = 0.f;
+    auto step = [&](const Keys& w, const Place& p, const Place& q) LC_INLINE {
+        sum += shares(w, p.r, p.hi);
+        if (q.e != p.e) {
+            const float all = total(sum) + __int_as_float(lc_readlane(__float_as_int(so_far), p.e));
+            const int chunk = lc_readlane(id, p.e);
+            if (lane == 0) weights[chunk] = all;
+            sum = 0.f;
+        }
+    };
+    if (p.e < n_e) {
+        Keys x, y;
+        load(x, p.r, p.hi);
+        for (;;) {
+            const Place q = next(p);
+            load(y, q.r, q.hi);
+            __builtin_amdgcn_sched_barrier(0);
+            step(x, p, q);
+            if (q.e >= n_e) break;
+            p = next(q);
+            load(x, p.r, p.hi);
+            __builtin_amdgcn_sched_barrier(0);
+            step(y, q, p);
+            if (p.e >= n_e) break;
+        }
+    }
+    // long chunks: a step of each wavefront in turn
+    unsigned long long longs = __ballot(begin_short != begin);
+    while (longs != 0ull) {
+        const int e = __ffsll((long long)longs) - 1;
+        longs &= longs - 1ull;
+        const int lo = lc_readlane(begin, e), hi = lc_readlane(end, e);
+        float mine = 0.f;
+        Keys x, y;
+        load(x, lo + wave * LC_WG_ROWS, hi);
+        for (int r = lo + wave * LC_WG_ROWS; r < hi; r += 2 * LC_WG_WAVES * LC_WG_ROWS) {
+            load(y, r + LC_WG_WAVES * LC_WG_ROWS, hi);
+            __builtin_amdgcn_sched_barrier(0);
+            mine += shares(x, r, hi);
+            load(x, r + 2 * LC_WG_WAVES * LC_WG_ROWS, hi);
+            __builtin_amdgcn_sched_barrier(0);
+            mine += shares(y, r + LC_WG_WAVES * LC_WG_ROWS, hi);
+        }
+        mine = total(mine);
+        if (lane == 0) part_sh[wave] = mine;
+        __syncthreads();
+        const float all = (part_sh[0] + part_sh[1]) + (part_sh[2] + part_sh[3]);
+        if (tid == 0) weights[lc_readlane(id, e)] = all + __int_as_float(lc_readlane(__float_as_int(so_far), e));
+        __syncthreads();
     }
 }
 
 template <bool IN4>
-int launch_weigh(const LcWeighArgs& a, int G, hipStream_t stream) {
-    // a chunk to a wavefront while there are chunks for some thousand of them
-    const int B = a.ix.B, H = a.ix.H;
-    const int parts_all = (a.cap + LC_WG_WAVES - 1) / LC_WG_WAVES;
-    const int fit = (16 * LC_COMPUTE_UNITS + B * H - 1) / (B * H);
-    const dim3 grid(parts_all < fit ? parts_all : fit, H, B);
-    switch (G) {
-        case 1: hipLaunchKernelGGL((lc_weigh_kernel<1, IN4>), grid, dim3(LC_WG_THREADS), 0, stream, a); break;
-        case 2: hipLaunchKernelGGL((lc_weigh_kernel<2, IN4>), grid, dim3(LC_WG_THREADS), 0, stream, a); break;
-        case 3: hipLaunchKernelGGL((lc_weigh_kernel<3, IN4>), grid, dim3(LC_WG_THREADS), 0, stream, a); break;
-        case 4: hipLaunchKernelGGL((lc_weigh_kernel<4, IN4>), grid, dim3(LC_WG_THREADS), 0, stream, a); break;
-        case 5: hipLaunchKernelGGL((lc_weigh_kernel<5, IN4>), grid, dim3(LC_WG_THREADS), 0, stream, a); break;
-        case 6: hipLaunchKernelGGL((lc_weigh_kernel<6, IN4>), grid, dim3(LC_WG_THREADS), 0, stream, a); break;
-        case 7: hipLaunchKernelGGL((lc_weigh_kernel<7, IN4>), grid, dim3(LC_WG_THREADS), 0, stream, a); break;
-        default: hipLaunchKernelGGL((lc_weigh_kernel<8, IN4>), grid, dim3(LC_WG_THREADS), 0, stream, a); break;
-    }
+int launch_weigh(LcWeighArgs& a, hipStream_t stream) {
+    // a chunk to a wavefront while that fills the device, then up to 16 of them, whose first loads are then shared
+    const long long entries = (long long)a.cap * a.ix.B * a.ix.H;
+    long long each = (entries + LC_WG_WAVES_FULL - 1) / LC_WG_WAVES_FULL;
+    if (each > 16) each = 16;
+    a.per = LC_WG_WAVES * (int)each;
+    hipLaunchKernelGGL((lc_weigh_kernel<IN4>), dim3((a.cap + a.per - 1) / a.per, a.ix.H, a.ix.B), dim3(LC_WG_THREADS), 0, stream, a);
     LC_HIP_CHECK(hipGetLastError());
     return LC_OK;
 }
@@ -597,7 +652,8 @@ int weigh(const lc_index* idx, const void* q, const void* K, const int64_t s[3],
     a.cap = cap;
     a.lse = lse;
     a.weights = weights;
-    return in4 ? launch_weigh<true>(a, H_q / idx->H_kv, static_cast<hipStream_t>(stream)) : launch_weigh<false>(a, H_q / idx->H_kv, static_cast<hipStream_t>(stream));
+    a.G = H_q / idx->H_kv;
+    return in4 ? launch_weigh<true>(a, static_cast<hipStream_t>(stream)) : launch_weigh<false>(a, static_cast<hipStream_t>(stream));
 }
 
 int evict_rows(const lc_index* idx, const int32_t* keep_ids, const int32_t* keep_bounds, const int32_t* keep_counts, const void* K, const void* V,
