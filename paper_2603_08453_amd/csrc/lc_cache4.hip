@@ -138,7 +138,7 @@ lc_decode4_kernel(const LcDecode4Args a) {
     };
     __shared__ __attribute__((aligned(16))) Phases ph;
     __shared__ __attribute__((aligned(16))) int off_sh[E * LC_D4_THREADS + 4], st_sh[E * LC_D4_THREADS];
-    __shared__ int scan_sh[8];
+    __shared__ int scan_sh[8], slot_sh[64];
     __shared__ int first_sh, last_sh;
 
     const LcDev& ix = a.ix;
@@ -157,12 +157,14 @@ lc_decode4_kernel(const LcDecode4Args a) {
 
     // ---- the attended tokens: the listed chunks in the list's order, then the open tail.  Thread t of a pass owns entries [E t, E t + E);
     // the first pass stays in registers.
-    lc_v4i idv[E / 4];
-    auto load_ids = [&](int base) LC_INLINE {
+    struct Ids { lc_v4i v[E / 4]; };
+    auto load_ids = [&](int base) LC_INLINE -> Ids {
+        Ids w;
 #pragma unroll
-        for (int e = 0; e < E / 4; ++e) idv[e] = __builtin_amdgcn_raw_buffer_load_b128(ids_r, (base + tid * E) * 4, 16 * e, 0);
+        for (int e = 0; e < E / 4; ++e) w.v[e] = __builtin_amdgcn_raw_buffer_load_b128(ids_r, (base + tid * E) * 4, 16 * e, 0);
+        return w;
     };
-    load_ids(0);
+    const Ids ids0 = load_ids(0);
     uint4 qb[4];
     {
         const uint16_t* qh = a.q + ((size_t)b * ix.H * G + (size_t)h * G + head) * LC_D + 32 * kg;
@@ -173,11 +175,11 @@ lc_decode4_kernel(const LcDecode4Args a) {
     const int n_ids = max(0, min(a.counts[bh], a.cap));
     const int tail_st = lc_buf_load_i32(bnd_r, M), tail_ln = max(0, T - tail_st);
     // (an entry that is no chunk holds no tokens)
-    auto entries = [&](int base, int (&st)[E], int (&ln)[E]) LC_INLINE -> int {
+    auto entries = [&](const Ids& ids, int base, int (&st)[E], int (&ln)[E]) LC_INLINE -> int {
         int sum = 0;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const int id = idv[e / 4][e % 4];
+            const int id = ids.v[e / 4][e % 4];
             const bool real = base + tid * E + e < n_ids && id >= 0 && id < M;
             // (branch-free: a load past the resource's end gives zeros)
             const lc_v2i x = __builtin_amdgcn_raw_buffer_load_b64(bnd_r, real ? id * 4 : 0x7ffffff0, 0, 0);
@@ -192,13 +194,25 @@ lc_decode4_kernel(const LcDecode4Args a) {
         return sum;
     };
     int st0[E], ln0[E], tot0;
-    const int ex0 = lc_block_scan<LC_D4_THREADS>(entries(0, st0, ln0), scan_sh, &tot0);
-    int n_sel = tot0;
-    for (int base = PASS; base < n_ids; base += PASS) {
-        int st[E], ln[E], tot;
-        load_ids(base);
-        lc_block_scan<LC_D4_THREADS>(entries(base, st, ln), scan_sh, &tot);
-        n_sel += tot;
+    if (tid < 64) slot_sh[tid] = 0;
+    const int ex0 = lc_block_scan<LC_D4_THREADS>(entries(ids0, 0, st0, ln0), scan_sh, &tot0);
+    // A longer list: the tokens of each of up to 64 slots of passes, so that a tile's rows are looked for in its own passes alone.
+    const bool long_list = n_ids > PASS;
+    const int passes = (n_ids + PASS - 1) / PASS, per_slot = (passes + 63) / 64;
+    int n_sel = tot0, slot_end = 0;                          // (lane l: tokens up to the end of slot l)
+    if (long_list) {
+        Ids next = load_ids(PASS);
+        for (int p = 1; p < passes; ++p) {
+            const Ids now = next;
+            if (p + 1 < passes) next = load_ids((p + 1) * PASS);
+            int st[E], ln[E];
+            const int sum = lc_wave_scan_incl(entries(now, p * PASS, st, ln));
+            if (lane == 63) atomicAdd(&slot_sh[p / per_slot], sum);
+        }
+        if (tid == 0) atomicAdd(&slot_sh[0], tot0);
+        __syncthreads();
+        slot_end = lc_wave_scan_incl(slot_sh[lane]);
+        n_sel = lc_readlane(slot_end, 63);
     }
     const int n_tok = n_sel + tail_ln;
     const int S_eff = max(1, min(S, (n_tok + LC_D4_MIN_TOKENS - 1) / LC_D4_MIN_TOKENS));
@@ -360,14 +374,18 @@ lc_decode4_kernel(const LcDecode4Args a) {
             }
         };
         if (tile0 != lo) __syncthreads();                           // the previous tile's rows have been used
-        place(0, ex0, tot0, min(n_ids, PASS), st0, ln0);
-        int carry = tot0;
-        for (int base = PASS; base < n_ids; base += PASS) {
-            int st[E], ln[E], tot;
-            load_ids(base);
-            const int ex = lc_block_scan<LC_D4_THREADS>(entries(base, st, ln), scan_sh, &tot);
-            place(carry, ex, tot, min(n_ids - base, PASS), st, ln);
-            carry += tot;
+        if (!long_list) {
+            place(0, ex0, tot0, n_ids, st0, ln0);
+        } else {
+            const unsigned long long behind = __ballot(slot_end > tile0);
+            const int slot = behind != 0ull ? __ffsll((long long)behind) - 1 : 64;
+            int carry = slot == 64 ? n_sel : slot == 0 ? 0 : lc_readlane(slot_end, slot - 1);
+            for (int p = slot * per_slot; p < passes && carry < tile0 + tl; ++p) {
+                int st[E], ln[E], tot;
+                const int ex = lc_block_scan<LC_D4_THREADS>(entries(load_ids(p * PASS), p * PASS, st, ln), scan_sh, &tot);
+                place(carry, ex, tot, min(n_ids - p * PASS, PASS), st, ln);
+                carry += tot;
+            }
         }
         for (int k = max(n_sel, tile0) + tid; k < tile0 + tl; k += LC_D4_THREADS) ph.row[k - tile0] = min(tail_st + (k - n_sel), row_max) * a.tok;
         // Rounds of a step per wavefront; each fetches its rows while the round before is computed, without a branch around the loads (behind one the wait for
@@ -622,6 +640,11 @@ int lc_sparse_decode4(const lc_index* idx, const void* q, const void* K4, const 
     a.part_ml = w.part_ml;
     a.out = out;
     a.lse = lse;
+    // splits that can find work at the index's length (the others would only read the list)
+    int most = 1;
+    for (int b = 0; b < idx->B; ++b) most = idx->T[b] > most ? idx->T[b] : most;
+    const int useful = (most + LC_D4_MIN_TOKENS - 1) / LC_D4_MIN_TOKENS;
+    if (useful < splits) splits = useful;
     hipStream_t st = static_cast<hipStream_t>(stream);
     switch (G) {
         case 1: return launch_decode4<1>(a, splits, st);

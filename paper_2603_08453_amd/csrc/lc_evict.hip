@@ -307,9 +307,20 @@ lc_evict_select_kernel(const LcEvictArgs a) {
 #pragma unroll
         for (int c = 0; c < C; ++c)
             if (c * NT < M) f((live >> c) & 1u, tid + c * NT, len[c], key[c]);
-        for (int j = C * NT + tid; j < M; j += NT) {
-            const int begin = bnd[j], end = bnd[j + 1];
-            if (!pinned(begin, end)) f(1u, j, end - begin, key_of(j));
+        // (four at a time, their loads together)
+        for (int j0 = C * NT + tid; j0 < M; j0 += 4 * NT) {
+            int begin[4], end[4];
+            unsigned long long k[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int j = min(j0 + u * NT, M - 1);
+                begin[u] = bnd[j];
+                end[u] = bnd[j + 1];
+                k[u] = key_of(j);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (j0 + u * NT < M && !pinned(begin[u], end[u])) f(1u, j0 + u * NT, end[u] - begin[u], k[u]);
         }
     };
 
@@ -473,21 +484,33 @@ lc_evict_select_kernel(const LcEvictArgs a) {
         n_keep = found_sh[0];
         n_tok = found_sh[1];
     }
-    for (int j0 = C * NT; j0 < M; j0 += NT) {
-        const int j = j0 + tid;
-        bool keep = false;
+    // (a thread has four chunks in a row: a scan for 4096)
+    for (int j0 = C * NT; j0 < M; j0 += 4 * NT) {
+        const int j = j0 + 4 * tid;
+        int edge[5];
+        unsigned long long k[4];
+#pragma unroll
+        for (int u = 0; u < 5; ++u) edge[u] = bnd[min(j + u, M)];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) k[u] = all ? 0ull : key_of(min(j + u, M - 1));
+        uint32_t kept = 0u;
         int n = 0;
-        if (j < M) {
-            const int begin = bnd[j], end = bnd[j + 1];
-            n = end - begin;
-            keep = all || pinned(begin, end) || keeps(key_of(j), j);
-        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (j + u < M && (pinned(edge[u], edge[u + 1]) || keeps(k[u], j + u))) {
+                kept |= 1u << u;
+                n += edge[u + 1] - edge[u];
+            }
         int at, to, count, tokens;
-        lc_block_scan2<NT>(keep ? 1 : 0, keep ? n : 0, scan_sh, &at, &to, &count, &tokens);
-        if (keep) {
-            ids[n_keep + at] = j;
-            bounds[n_keep + at] = n_tok + to;
-        }
+        lc_block_scan2<NT>(__popc(kept), n, scan_sh, &at, &to, &count, &tokens);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if ((kept >> u) & 1u) {
+                ids[n_keep + at] = j + u;
+                bounds[n_keep + at] = n_tok + to;
+                at += 1;
+                to += edge[u + 1] - edge[u];
+            }
         n_keep += count;
         n_tok += tokens;
     }

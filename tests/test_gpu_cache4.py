@@ -128,6 +128,16 @@ def test_long_lists_and_long_chunks(C):
         c.check(qb, ids, out, lse)
 
 
+def test_a_list_of_more_passes_than_slots(C):
+    """140000 chunks of one token: the list is read in 69 passes, two of them to a slot."""
+    n = 140000
+    c = C.Cache(33, 1, 2, [n + 3], [np.arange(n + 1)], levels=1)
+    qb = c.query()
+    for ids in ([[np.arange(n)]], [[np.concatenate([np.arange(100), np.arange(135000, n, 2)])]]):
+        out, lse = c.attend(qb, ids)
+        c.check(qb, ids, out, lse)
+
+
 @pytest.mark.parametrize("G", [2, 7])
 def test_rows_that_attend_to_nothing(C, G):
     r = np.random.default_rng(6)
