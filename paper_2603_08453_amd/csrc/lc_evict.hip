@@ -528,7 +528,8 @@ lc_evict_select_kernel(const LcEvictArgs a) {
 // ---------------------------------------------------------------- the rows that stay
 #define LC_ER_THREADS 256
 #define LC_ER_ROWS 64             // new rows of a tile
-#define LC_ER_GROUPS 4096         // workgroups for rows at most; each goes on to further tiles
+#define LC_ER_STREAM (32LL << 20)         // bytes of keys and values from which on bfloat16 rows go past the caches
+#define LC_ER_GROUPS 65536        // workgroups for rows at most; each goes on to further tiles
 
 struct LcEvictRowsArgs {
     LcDev ix;
@@ -545,11 +546,13 @@ struct LcEvictRowsArgs {
 // The piece of a 4-bit row that a lane moves at a time: rows are 4-byte aligned.
 typedef int LcPiece4 __attribute__((ext_vector_type(4), aligned(4)));
 
-// A tile is ROWS new rows of a (sequence, head), keys and values: the rows of the kept chunks one behind the other, then the open tail's.  Bound by the
-// bytes where chunks are long (16 K of 32 K tokens of 4 sequences, 8 heads, bfloat16: 538 MB in 114 us); chunks of a dozen tokens in 4 bits are runs of 0.8 KB,
-// which the memory reads at 3.1 TB/s of useful bytes.  Before those a tile has a chain of five loads to find its rows.  (Tiles of 128 and 256 rows in 4
-// bits: 24.6 and 28.3 us where 64 take 23.0; several heads to a workgroup, which share the rows' places: 23.9 to 26.6, bfloat16 116.)
-template <int BYTES, int ROWS>    // bytes of a row
+// A tile is ROWS new rows of a (sequence, head), keys and values: the rows of the kept chunks one behind the other, then the open tail's; a chain of five loads
+// finds them.  Bound by the bytes where chunks are long: half of 32K tokens of 4 sequences, 8 heads, bfloat16, 538 MB, in 95 us (5.7 TB/s; through the caches 114,
+// with 4096 workgroups that go on to further tiles instead of a tile each 102), of one sequence 27 us (33 through the caches; half of 8K tokens, 34 MB: 9.7 either way,
+// a quarter of 4K 4.9 through them, 6.0 past them).  Chunks of a dozen tokens in 4 bits are runs of 0.8 KB, which the memory reads at 3.1 TB/s of useful bytes: 128K
+// tokens cut to a quarter 23 us.  (There tiles of 128 and 256 rows take 24.6 and 28.3; past the caches, where rows share lines, 32; several heads to a workgroup, which share
+// the rows' places, 23.9 to 26.6.)
+template <int BYTES, int ROWS, bool STREAM>    // bytes of a row; past the caches
 __global__ void __launch_bounds__(LC_ER_THREADS)
 lc_evict_rows_kernel(const LcEvictRowsArgs a) {
     lc_fetch_args<sizeof(LcEvictRowsArgs)>();
@@ -617,8 +620,13 @@ lc_evict_rows_kernel(const LcEvictRowsArgs a) {
             const int i = tid + u * LC_ER_THREADS, r = i / PIECES;
             if (r < m) {
                 const size_t f = from + (size_t)row_sh[r] * a.tok + i % PIECES * 16;
-                k[u] = *reinterpret_cast<const Piece*>(a.K + f);
-                v[u] = *reinterpret_cast<const Piece*>(a.V + f);
+                if constexpr (STREAM) {
+                    k[u] = __builtin_nontemporal_load(reinterpret_cast<const Piece*>(a.K + f));
+                    v[u] = __builtin_nontemporal_load(reinterpret_cast<const Piece*>(a.V + f));
+                } else {
+                    k[u] = *reinterpret_cast<const Piece*>(a.K + f);
+                    v[u] = *reinterpret_cast<const Piece*>(a.V + f);
+                }
             }
         }
         if (BYTES % 16 != 0 && tid < m) {
@@ -631,8 +639,13 @@ lc_evict_rows_kernel(const LcEvictRowsArgs a) {
             const int i = tid + u * LC_ER_THREADS, r = i / PIECES;
             if (r < m) {
                 const size_t t = to + (size_t)(r0 + r) * a.tok_to + i % PIECES * 16;
-                *reinterpret_cast<Piece*>(a.K_to + t) = k[u];
-                *reinterpret_cast<Piece*>(a.V_to + t) = v[u];
+                if constexpr (STREAM) {
+                    __builtin_nontemporal_store((Piece)k[u], reinterpret_cast<Piece*>(a.K_to + t));
+                    __builtin_nontemporal_store((Piece)v[u], reinterpret_cast<Piece*>(a.V_to + t));
+                } else {
+                    *reinterpret_cast<Piece*>(a.K_to + t) = k[u];
+                    *reinterpret_cast<Piece*>(a.V_to + t) = v[u];
+                }
             }
         }
         if (BYTES % 16 != 0 && tid < m) {
@@ -707,8 +720,12 @@ int evict_rows(const lc_index* idx, const int32_t* keep_ids, const int32_t* keep
     const int weight_tiles = weights ? (idx->cfg.max_chunks + LC_ER_THREADS - 1) / LC_ER_THREADS : 0;
     const dim3 grid(a.row_tiles + weight_tiles, idx->H_kv, idx->B);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (in4) hipLaunchKernelGGL((lc_evict_rows_kernel<LC_ROW4, LC_ER_ROWS>), grid, dim3(LC_ER_THREADS), 0, st, a);
-    else hipLaunchKernelGGL((lc_evict_rows_kernel<2 * LC_D, LC_ER_ROWS>), grid, dim3(LC_ER_THREADS), 0, st, a);
+    long long rows = 0;
+    for (int b = 0; b < idx->B; ++b) rows += idx->T[b];
+    const dim3 block(LC_ER_THREADS);
+    if (in4) hipLaunchKernelGGL((lc_evict_rows_kernel<LC_ROW4, LC_ER_ROWS, false>), grid, block, 0, st, a);
+    else if (rows * idx->H_kv * (4 * LC_D) > LC_ER_STREAM) hipLaunchKernelGGL((lc_evict_rows_kernel<2 * LC_D, LC_ER_ROWS, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((lc_evict_rows_kernel<2 * LC_D, LC_ER_ROWS, false>), grid, block, 0, st, a);
     LC_HIP_CHECK(hipGetLastError());
     return LC_OK;
 }
