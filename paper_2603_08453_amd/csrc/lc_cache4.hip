@@ -4,7 +4,7 @@
 // Attention.  With x_t = q.k_t / sqrt(d) over the tokens of the listed chunks and of the open tail,
 //   out = sum_t e^(x_t - m) v_t / sum_t e^(x_t - m),   lse = m + ln sum_t e^(x_t - m),
 // in one pass over the rows: each wavefront keeps a reference m of its own (a whole number of powers of two, not below its largest logit so far), the
-// parts meet at the end.  Grid (split, KV head, sequence), 256 threads; a wavefront takes 32 tokens at a time.
+// parts meet at the end.  Grid (KV head, sequence, split), 256 threads; a wavefront takes 32 tokens at a time.
 //   Q.K^T: the 16 tokens of half a step are the rows of a 16x16x32 bf16 product's A operand, lane (kg, n) holding the 32 columns [32 kg, ...) of
 //   row n -- one 16-byte load, whose scale is one byte -- as four operands of eight; the query block is the B operand.  The products leave lane
 //   (kg, n) the logits of tokens 4 kg .. 4 kg + 3 for the head of column n.
@@ -45,7 +45,7 @@ struct LcMove4Args {
 // Row i of the sequence's range: from row i of K or V to row first + i of K4 or V4.  16 lanes to a row, 64 rows to a workgroup; z: keys and values of
 // each sequence in turn.  Bound by the bytes: 128K tokens of 8 heads, 680 MB, are stored in 116 us and loaded in 115 (5.9 TB/s).  The bfloat16 side, which nobody
 // reads again soon, goes past the caches: 64K tokens are stored in 54 us (60 through them) and loaded in 50 (63).  Writing 16 bytes a lane, by way of
-// LDS, was no faster than four.
+// LDS, was no faster than four; with the heads of a tile one after the other instead of the tiles of a head 128K tokens took 124 and 127.
 __global__ void __launch_bounds__(LC_C4_THREADS)
 lc_store4_kernel(const LcMove4Args a) {
     const int b = blockIdx.z >> 1, h = blockIdx.y, sub = threadIdx.x & 15, grp = threadIdx.x >> 4;
@@ -144,7 +144,7 @@ lc_decode4_kernel(const LcDecode4Args a) {
     __shared__ int first_sh, last_sh;
 
     const LcDev& ix = a.ix;
-    const int s = blockIdx.x, S = gridDim.x, h = blockIdx.y, b = blockIdx.z;
+    const int s = blockIdx.z, S = gridDim.z, h = blockIdx.x, b = blockIdx.y;
     const int bh = b * ix.H + h;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, kg = lane >> 4;
     // the head and the term of this lane's column
@@ -539,7 +539,7 @@ lc_decode4_kernel(const LcDecode4Args a) {
 
 template <int G>
 int launch_decode4(const LcDecode4Args& a, int splits, hipStream_t stream) {
-    hipLaunchKernelGGL((lc_decode4_kernel<G>), dim3(splits, a.ix.H, a.ix.B), dim3(LC_D4_THREADS), 0, stream, a);
+    hipLaunchKernelGGL((lc_decode4_kernel<G>), dim3(a.ix.H, a.ix.B, splits), dim3(LC_D4_THREADS), 0, stream, a);
     LC_HIP_CHECK(hipGetLastError());
     return LC_OK;
 }

@@ -12,7 +12,7 @@
 #define LC_WG_WAVES (LC_WG_THREADS / 64)
 #define LC_WG_LONG 512            // tokens from which on a chunk is shared by the workgroup's wavefronts
 #define LC_WG_ROWS 32             // tokens of a step
-#define LC_WG_WAVES_FULL 8192     // wavefronts up to which each has one chunk
+#define LC_WG_GROUPS 2048         // workgroups at most (rounded up to whole pairs)
 
 namespace {
 
@@ -33,28 +33,30 @@ struct LcWeighArgs {
     const float* lse;     // [B][H*G]
     float* weights;       // [B][H][cap0]
     int G;                // heads of a group
-    int per;              // list entries of a workgroup, at most 64
 };
 
 //
-// A workgroup has `per` (up to 64) entries of a list, whose chunks, boundaries and weights so far come in one go, a lane to an entry; a wavefront takes every fourth of them
-// and goes through their tokens 32 at a time, the next step's keys on their way, the next chunk's behind a chunk's last.
+// A workgroup has some entries of a list, whose chunks, boundaries and weights so far come in one go, a lane to an entry, 64 at a time; a wavefront takes every fourth of
+// them and goes through their tokens 32 at a time, the next step's keys on their way, the next chunk's behind a chunk's last.
 template <bool IN4>
 __global__ void __launch_bounds__(LC_WG_THREADS)
 lc_weigh_kernel(const LcWeighArgs a) {
     lc_fetch_args<sizeof(LcWeighArgs)>();
     __shared__ float part_sh[LC_WG_WAVES];
     const LcDev& ix = a.ix;
-    const int h = blockIdx.y, b = blockIdx.z, bh = b * ix.H + h;
+    const int h = blockIdx.x, b = blockIdx.y, bh = b * ix.H + h, part = blockIdx.z, parts = gridDim.z;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, kg = lane >> 4;
     const int G = a.G, head = min(n, G - 1);
-    const int e0 = (int)blockIdx.x * a.per;
-    // this lane's entry, and the one before
+    // The entries are dealt evenly, a chunk to a wavefront at least.  How many there are the device knows alone (a list's table may have room for
+    // far more): the first ones are on their way before the count is there, and the workgroups without entries are the last ones of all (as the last ones
+    // of each pair they left the others on a few compute units: 12.0 us instead of 6.0 with room for 512 and more where 85 were listed).
     const __amdgpu_buffer_rsrc_t ids_r = lc_buffer(a.ids + (size_t)bh * a.cap, (int)(min((long long)a.cap, 1LL << 28) * 4));
-    const int id = lc_buf_load_i32(ids_r, e0 + lane), before = e0 + lane > 0 ? lc_buf_load_i32(ids_r, e0 + lane - 1) : -1;
+    const int guess = part * LC_WG_WAVES;
+    int id = lc_buf_load_i32(ids_r, guess + lane), before = lc_buf_load_i32(ids_r, max(0, guess + lane - 1));
     const int count = max(0, min(a.counts[bh], a.cap)), M = ix.state[bh * 4 + 1];
-    const int n_e = min(a.per, count - e0);
-    if (n_e <= 0) return;
+    const int per = max(LC_WG_WAVES, (count + parts - 1) / parts);
+    const int e_lo = part * per, e_hi = min(count, e_lo + per);
+    if (e_lo >= e_hi) return;
     // the query block as in the attention (bfloat16 rows: lane (kg, n) has columns 8 kg + 32 j, 4-bit rows: 32 kg + 8 j)
     uint4 qb[4];
     {
@@ -64,14 +66,7 @@ lc_weigh_kernel(const LcWeighArgs a) {
     }
     const float lse = a.lse[(size_t)bh * G + head];
     float* weights = a.weights + (size_t)bh * ix.cap[0];
-    // (an entry that is no chunk, or no larger than the one before it, is passed over: it has no tokens)
-    const bool real = lane < n_e && id >= 0 && id < M && id > before;
     const int* bnd = ix.bounds + (size_t)b * (ix.cap[0] + 1);
-    const int at = real ? id : 0;
-    const int begin = bnd[at], end = real ? min(bnd[at + 1], a.max_tokens) : begin;
-    const float so_far = weights[at];
-    const int begin_short = end - begin < LC_WG_LONG ? begin : end;      // long chunks are done behind the others
-
     const float scale = 0.08838834764831845f * LC_LOG2E;
     const float off = lse == LC_NEG_INF ? LC_NEG_INF : -lse * LC_LOG2E;      // (a head that attended to nothing adds nothing)
     constexpr int ROW = IN4 ? LC_ROW4 : 2 * LC_D, HALVES = LC_WG_ROWS / 16, PIECES = IN4 ? 1 : 4;
@@ -83,7 +78,7 @@ lc_weigh_kernel(const LcWeighArgs a) {
     auto load = [&](Keys& w, int r, int hi) LC_INLINE {
 #pragma unroll
         for (int t = 0; t < HALVES; ++t) {
-            const int row = r + 16 * t + n, o = row < hi ? row * a.tok + 16 * kg : slab_bytes;
+            const int row = r + 16 * t + n, o = row < hi ? (int)((uint32_t)row * (uint32_t)a.tok) + 16 * kg : slab_bytes;
 #pragma unroll
             for (int j = 0; j < PIECES; ++j) w.k[t][j] = __builtin_amdgcn_raw_buffer_load_b128(Kr, o, 64 * j, 0);
             w.s[t] = IN4 ? lc_buf_load_u8(Kr, o + 64 - 15 * kg) : 0;
@@ -113,86 +108,95 @@ lc_weigh_kernel(const LcWeighArgs a) {
         return lc_add_rows(sum, sum);
     };
 
-    // the wavefront's steps: entry, first row, the chunk's end
-    struct Place { int e, r, hi; };
-    auto settle = [&](Place& p) LC_INLINE {                    // from the beginning of an entry to one with tokens
-        for (; p.e < n_e; p.e += LC_WG_WAVES) {
-            p.r = lc_readlane(begin_short, p.e);
-            p.hi = lc_readlane(end, p.e);
-            if (p.r < p.hi) return;
+    for (int e0 = e_lo; e0 < e_hi; e0 += 64) {
+        const int n_e = min(64, e_hi - e0);
+        if (e0 != guess) {
+            id = lc_buf_load_i32(ids_r, e0 + lane);
+            before = lc_buf_load_i32(ids_r, max(0, e0 + lane - 1));
         }
-        p.r = p.hi = 0;
-    };
-    auto next = [&](const Place& p) LC_INLINE -> Place {
-        Place q = {p.e, p.r + LC_WG_ROWS, p.hi};
-        if (q.r >= q.hi) {
-            q.e += LC_WG_WAVES;
-            settle(q);
-        }
-        return q;
-    };
-    Place p = {wave, 0, 0};
-    settle(p);
-    float sum = 0.f;
-    auto step = [&](const Keys& w, const Place& p, const Place& q) LC_INLINE {
-        sum += shares(w, p.r, p.hi);
-        if (q.e != p.e) {
-            const float all = total(sum) + __int_as_float(lc_readlane(__float_as_int(so_far), p.e));
-            const int chunk = lc_readlane(id, p.e);
-            if (lane == 0) weights[chunk] = all;
-            sum = 0.f;
-        }
-    };
-    if (p.e < n_e) {
-        Keys x, y;
-        load(x, p.r, p.hi);
-        for (;;) {
-            const Place q = next(p);
-            load(y, q.r, q.hi);
-            __builtin_amdgcn_sched_barrier(0);
-            step(x, p, q);
-            if (q.e >= n_e) break;
-            p = next(q);
+        // (an entry that is no chunk, or no larger than the one before it, is passed over: it has no tokens)
+        const bool real = lane < n_e && id >= 0 && id < M && (e0 + lane == 0 || id > before);
+        const int at = real ? id : 0;
+        const int begin = bnd[at], end = real ? min(bnd[at + 1], a.max_tokens) : begin;
+        const float so_far = weights[at];
+        const int begin_short = end - begin < LC_WG_LONG ? begin : end;      // long chunks are done behind the others
+        // the wavefront's steps: entry, first row, the chunk's end
+        struct Place { int e, r, hi; };
+        auto settle = [&](Place& p) LC_INLINE {                    // from the beginning of an entry to one with tokens
+            for (; p.e < n_e; p.e += LC_WG_WAVES) {
+                p.r = lc_readlane(begin_short, p.e);
+                p.hi = lc_readlane(end, p.e);
+                if (p.r < p.hi) return;
+            }
+            p.r = p.hi = 0;
+        };
+        auto next = [&](const Place& p) LC_INLINE -> Place {
+            Place q = {p.e, p.r + LC_WG_ROWS, p.hi};
+            if (q.r >= q.hi) {
+                q.e += LC_WG_WAVES;
+                settle(q);
+            }
+            return q;
+        };
+        Place p = {wave, 0, 0};
+        settle(p);
+        float sum = 0.f;
+        auto step = [&](const Keys& w, const Place& p, const Place& q) LC_INLINE {
+            sum += shares(w, p.r, p.hi);
+            if (q.e != p.e) {
+                const float all = total(sum) + __int_as_float(lc_readlane(__float_as_int(so_far), p.e));
+                const int chunk = lc_readlane(id, p.e);
+                if (lane == 0) weights[chunk] = all;
+                sum = 0.f;
+            }
+        };
+        if (p.e < n_e) {
+            Keys x, y;
             load(x, p.r, p.hi);
-            __builtin_amdgcn_sched_barrier(0);
-            step(y, q, p);
-            if (p.e >= n_e) break;
+            for (;;) {
+                const Place q = next(p);
+                load(y, q.r, q.hi);
+                __builtin_amdgcn_sched_barrier(0);
+                step(x, p, q);
+                if (q.e >= n_e) break;
+                p = next(q);
+                load(x, p.r, p.hi);
+                __builtin_amdgcn_sched_barrier(0);
+                step(y, q, p);
+                if (p.e >= n_e) break;
+            }
         }
-    }
-    // long chunks: a step of each wavefront in turn
-    unsigned long long longs = __ballot(begin_short != begin);
-    while (longs != 0ull) {
-        const int e = __ffsll((long long)longs) - 1;
-        longs &= longs - 1ull;
-        const int lo = lc_readlane(begin, e), hi = lc_readlane(end, e);
-        float mine = 0.f;
-        Keys x, y;
-        load(x, lo + wave * LC_WG_ROWS, hi);
-        for (int r = lo + wave * LC_WG_ROWS; r < hi; r += 2 * LC_WG_WAVES * LC_WG_ROWS) {
-            load(y, r + LC_WG_WAVES * LC_WG_ROWS, hi);
-            __builtin_amdgcn_sched_barrier(0);
-            mine += shares(x, r, hi);
-            load(x, r + 2 * LC_WG_WAVES * LC_WG_ROWS, hi);
-            __builtin_amdgcn_sched_barrier(0);
-            mine += shares(y, r + LC_WG_WAVES * LC_WG_ROWS, hi);
+        // long chunks: a step of each wavefront in turn
+        unsigned long long longs = __ballot(begin_short != begin);
+        while (longs != 0ull) {
+            const int e = __ffsll((long long)longs) - 1;
+            longs &= longs - 1ull;
+            const int lo = lc_readlane(begin, e), hi = lc_readlane(end, e);
+            float mine = 0.f;
+            Keys x, y;
+            load(x, lo + wave * LC_WG_ROWS, hi);
+            for (int r = lo + wave * LC_WG_ROWS; r < hi; r += 2 * LC_WG_WAVES * LC_WG_ROWS) {
+                load(y, r + LC_WG_WAVES * LC_WG_ROWS, hi);
+                __builtin_amdgcn_sched_barrier(0);
+                mine += shares(x, r, hi);
+                load(x, r + 2 * LC_WG_WAVES * LC_WG_ROWS, hi);
+                __builtin_amdgcn_sched_barrier(0);
+                mine += shares(y, r + LC_WG_WAVES * LC_WG_ROWS, hi);
+            }
+            mine = total(mine);
+            if (lane == 0) part_sh[wave] = mine;
+            __syncthreads();
+            const float all = (part_sh[0] + part_sh[1]) + (part_sh[2] + part_sh[3]);
+            if (tid == 0) weights[lc_readlane(id, e)] = all + __int_as_float(lc_readlane(__float_as_int(so_far), e));
+            __syncthreads();
         }
-        mine = total(mine);
-        if (lane == 0) part_sh[wave] = mine;
-        __syncthreads();
-        const float all = (part_sh[0] + part_sh[1]) + (part_sh[2] + part_sh[3]);
-        if (tid == 0) weights[lc_readlane(id, e)] = all + __int_as_float(lc_readlane(__float_as_int(so_far), e));
-        __syncthreads();
     }
 }
 
 template <bool IN4>
 int launch_weigh(LcWeighArgs& a, hipStream_t stream) {
-    // a chunk to a wavefront while that fills the device, then up to 16 of them, whose first loads are then shared
-    const long long entries = (long long)a.cap * a.ix.B * a.ix.H;
-    long long each = (entries + LC_WG_WAVES_FULL - 1) / LC_WG_WAVES_FULL;
-    if (each > 16) each = 16;
-    a.per = LC_WG_WAVES * (int)each;
-    hipLaunchKernelGGL((lc_weigh_kernel<IN4>), dim3((a.cap + a.per - 1) / a.per, a.ix.H, a.ix.B), dim3(LC_WG_THREADS), 0, stream, a);
+    const int pairs = a.ix.B * a.ix.H, all = (a.cap + LC_WG_WAVES - 1) / LC_WG_WAVES, fit = (LC_WG_GROUPS + pairs - 1) / pairs;
+    hipLaunchKernelGGL((lc_weigh_kernel<IN4>), dim3(a.ix.H, a.ix.B, all < fit ? all : fit), dim3(LC_WG_THREADS), 0, stream, a);
     LC_HIP_CHECK(hipGetLastError());
     return LC_OK;
 }
@@ -529,7 +533,8 @@ lc_evict_select_kernel(const LcEvictArgs a) {
 #define LC_ER_THREADS 256
 #define LC_ER_ROWS 64             // new rows of a tile
 #define LC_ER_STREAM (32LL << 20)         // bytes of keys and values from which on bfloat16 rows go past the caches
-#define LC_ER_GROUPS 65536        // workgroups for rows at most; each goes on to further tiles
+#define LC_ER_GROUPS 32768        // workgroups for rows at most; each goes on to further tiles
+#define LC_ER_WEIGHTS 64          // workgroups of a (sequence, head) for weights at most
 #define LC_ER_GROUPS4 4096        // ... in 4 bits, where a tile is a few KB and those past the kept rows' end are not free (25 us without, 23 with)
 
 struct LcEvictRowsArgs {
@@ -549,7 +554,7 @@ typedef int LcPiece4 __attribute__((ext_vector_type(4), aligned(4)));
 
 // A tile is ROWS new rows of a (sequence, head), keys and values: the rows of the kept chunks one behind the other, then the open tail's; a chain of five loads
 // finds them.  Bound by the bytes where chunks are long: half of 32K tokens of 4 sequences, 8 heads, bfloat16, 538 MB, in 95 us (5.7 TB/s; through the caches 114,
-// with 4096 workgroups that go on to further tiles instead of a tile each 102), of one sequence 27 us (33 through the caches; half of 8K tokens, 34 MB: 9.7 either way,
+// with 4096 workgroups that go on to further tiles instead of a tile each 102, with the heads of a tile one after the other 102), of one sequence 27 us (33 through the caches; half of 8K tokens, 34 MB: 9.7 either way,
 // a quarter of 4K 4.9 through them, 6.0 past them).  Chunks of a dozen tokens in 4 bits are runs of 0.8 KB, which the memory reads at 3.1 TB/s of useful bytes: 128K
 // tokens cut to a quarter 23 us.  (There tiles of 128 and 256 rows take 24.6 and 28.3; past the caches, where rows share lines, 32; several heads to a workgroup, which share
 // the rows' places, 23.9 to 26.6.)
@@ -560,23 +565,23 @@ lc_evict_rows_kernel(const LcEvictRowsArgs a) {
     __shared__ int bound_sh[ROWS], begin_sh[ROWS];
     __shared__ int row_sh[ROWS];
     const LcDev& ix = a.ix;
-    const int h = blockIdx.y, b = blockIdx.z, bh = b * ix.H + h, tid = threadIdx.x, lane = tid & 63;
+    const int h = blockIdx.y, b = blockIdx.z, bh = b * ix.H + h, part = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
     const int cap = ix.cap[0];
     const int32_t* ids = a.ids + (size_t)b * cap;
     const int32_t* kept = a.bounds + (size_t)b * (cap + 1);
     const int T = min(ix.state[bh * 4 + 0], a.max_tokens), M = min(ix.state[bh * 4 + 1], cap);
     const int* bnd = ix.bounds + (size_t)b * (cap + 1);
     const int n = max(0, min(a.counts[b], M));
-    if ((int)blockIdx.x >= a.row_tiles) {
-        const int i = ((int)blockIdx.x - a.row_tiles) * LC_ER_THREADS + tid;
-        if (i >= cap) return;
-        const int id = i < n ? ids[i] : -1;
-        a.weights_to[(size_t)bh * cap + i] = id >= 0 && id < M ? a.weights[(size_t)bh * cap + id] : 0.f;
+    if (part >= a.row_tiles) {
+        for (int i = (part - a.row_tiles) * LC_ER_THREADS + tid; i < cap; i += ((int)gridDim.x - a.row_tiles) * LC_ER_THREADS) {
+            const int id = i < n ? ids[i] : -1;
+            a.weights_to[(size_t)bh * cap + i] = id >= 0 && id < M ? a.weights[(size_t)bh * cap + id] : 0.f;
+        }
         return;
     }
     const int last = bnd[M], n_kept = max(0, min(kept[n], T)), rows = min(n_kept + max(0, T - last), a.max_tokens);
     const size_t from = (size_t)b * a.seq + (size_t)h * a.head, to = (size_t)b * a.seq_to + (size_t)h * a.head_to;
-    for (int r0 = blockIdx.x * ROWS; r0 < rows; r0 += a.row_tiles * ROWS) {
+    for (int r0 = part * ROWS; r0 < rows; r0 += a.row_tiles * ROWS) {
         // the last kept chunk that begins at or before r0: 64 boundaries at a time, each round a 64th of the range
         int lo = 0, len = n;                                 // boundaries lo .. lo + len - 1 are candidates, kept[lo] <= r0
         while (len > 1) {
@@ -718,7 +723,7 @@ int evict_rows(const lc_index* idx, const int32_t* keep_ids, const int32_t* keep
         if (idx->T[b] > most) most = idx->T[b];
     const int tiles = most > LC_ER_ROWS ? (most + LC_ER_ROWS - 1) / LC_ER_ROWS : 1, fit = ((in4 ? LC_ER_GROUPS4 : LC_ER_GROUPS) + idx->B * idx->H_kv - 1) / (idx->B * idx->H_kv);
     a.row_tiles = tiles < fit ? tiles : fit;
-    const int weight_tiles = weights ? (idx->cfg.max_chunks + LC_ER_THREADS - 1) / LC_ER_THREADS : 0;
+    const int slots = (idx->cfg.max_chunks + LC_ER_THREADS - 1) / LC_ER_THREADS, weight_tiles = weights ? (slots < LC_ER_WEIGHTS ? slots : LC_ER_WEIGHTS) : 0;
     const dim3 grid(a.row_tiles + weight_tiles, idx->H_kv, idx->B);
     hipStream_t st = static_cast<hipStream_t>(stream);
     long long rows = 0;
