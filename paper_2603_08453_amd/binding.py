@@ -484,6 +484,7 @@ def _move4(call, where, K, V, K4, V4, first, counts, stream, store):
     assert K.shape == V.shape and K.stride() == V.stride() and K4.shape == V4.shape and K4.stride() == V4.stride()
     assert K4.shape[:2] == K.shape[:2] and K.element_size() == 2
     counts = [rows] * B if counts is None else [int(n) for n in counts]
+    first = None if first is None else [int(n) for n in first]
     assert len(counts) == B and max(counts, default=0) <= rows and (first is None or len(first) == B)
     wide, narrow = (_ptr(K), _ptr(V), _strides3(K)), (_ptr(K4), _ptr(V4), _strides4(K4))
     range_ = (None if first is None else _i32(first), _i32(counts), B, H_kv, d)

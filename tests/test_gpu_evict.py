@@ -97,6 +97,29 @@ def test_weights_of_long_chunks_and_long_lists(C, bits):
     assert np.array_equal(_weigh(C, c, qb, ids, lse, before, bits), got)
 
 
+@pytest.mark.parametrize("bits", [16, 4])
+def test_weights_of_lists_longer_than_the_workgroups(C, bits):
+    """64 pairs share the workgroups: each has more entries than a wavefront has lanes; a table with room for more."""
+    n = 3000
+    c = C.Cache(52, 8, 1, [n + 7] * 8, [np.concatenate([np.arange(0, n - 600), np.arange(n - 600, n + 1, 3)])] * 8)
+    M = len(c.bounds[0]) - 1
+    ids = [[np.arange(h % 3, M, 1 + h % 2) for h in range(8)] for _ in range(8)]
+    keys = c.k4 if bits == 4 else (lambda b, h: wl.bf16_bits_to_f64(c.kb[b][h]))
+    qb = c.query()
+    lse = np.full((8, 8), 5.0, dtype=np.float32)
+    before = np.abs(c.r.standard_normal((8, 8, c.cfg.max_chunks))).astype(np.float32)
+    got = _weigh(C, c, qb, ids, lse, before, bits, c.table(ids, cap=M + 1500))
+    for b, h in ((0, 0), (3, 5), (7, 7)):
+        q, k = c.heads(qb, b, h), keys(b, h)
+        share = np.exp(k[:c.bounds[b][-1]] @ q[0] / math.sqrt(128) - 5.0)
+        want = before[b, h].astype(np.float64)
+        want[ids[b][h]] += np.add.reduceat(share, c.bounds[b][:-1])[ids[b][h]]
+        # as in _check_weights, with one head and at most three tokens
+        x = 130 * C.EPS * float((np.abs(k) @ np.abs(q[0])).max()) / math.sqrt(128)
+        x += 3 * C.EPS * (2 * x / (130 * C.EPS) + 5.0)
+        assert np.all(np.abs(got[b, h] - want) <= (math.expm1(x) + 16 * C.EPS) * (want - before[b, h]) + 2 * C.EPS * want), (b, h)
+
+
 def test_entries_and_heads_that_add_nothing(C):
     import torch
     c = C.Cache(51, 1, 3, [200], [np.arange(0, 201, 10)])
