@@ -184,7 +184,7 @@ lc_decode4_kernel(const LcDecode4Args a) {
         for (int c = 0; c < 4; ++c) qb[c] = *reinterpret_cast<const uint4*>(qh + 8 * c);
     }
     const int T = ix.state[bh * 4 + 0], M = ix.state[bh * 4 + 1];
-    const int n_ids = max(0, min(a.counts[bh], a.cap));
+    const int n_ids = max(0, min(a.counts[bh], min(a.cap, 1 << 28)));
     const int tail_st = lc_buf_load_i32(bnd_r, M), tail_ln = max(0, T - tail_st);
     // (an entry that is no chunk holds no tokens)
     auto entries = [&](const Ids& ids, int base, int (&st)[E], int (&ln)[E]) LC_INLINE -> int {

@@ -95,6 +95,32 @@ def test_ranges_of_many_sequences(C):
         assert (back[b, :, counts[b]:] == 3).all()
 
 
+@pytest.mark.parametrize("layout", ["bthd", "padded"])
+def test_bfloat16_rows_in_other_layouts(C, layout):
+    import torch
+    lc = C.lc
+    r = np.random.default_rng(14)
+    B, H, T = 2, 3, 150
+    bits = C.bf16_bits(r, B, H, T, 128)
+
+    def like(fill):
+        if layout == "bthd":
+            return torch.full((B, T, H, 128), fill, dtype=torch.bfloat16, device="cuda").transpose(1, 2)
+        return torch.full((B, H, T, 144), fill, dtype=torch.bfloat16, device="cuda")[..., 8:136]
+    K, V, Kb, Vb = like(0.0), like(0.0), like(9.0), like(9.0)
+    K.copy_(C.to_dev(bits))
+    V.copy_(C.to_dev(bits[::-1].copy()))
+    K4, V4 = (torch.zeros(B, H, T, 68, dtype=torch.uint8, device="cuda") for _ in range(2))
+    lc.lc_cache4_store(K, V, K4, V4, counts=[T, 70])
+    lc.lc_cache4_load(K4, V4, Kb, Vb, counts=[T - 1, 70])
+    torch.cuda.synchronize()
+    for x4, y, src in ((K4, Kb, bits), (V4, Vb, bits[::-1])):
+        for b, n, m in ((0, T, T - 1), (1, 70, 70)):
+            want = c4.pack(wl.bf16_bits_to_f64(src[b, 1, :n]))
+            assert np.array_equal(x4[b, 1, :n].cpu().numpy(), want) and not x4[b, 1, n:].any()
+            assert np.array_equal(y[b, 1, :m].float().cpu().numpy(), c4.unpack(want)[:m].astype(np.float32)) and (y[b, 1, m:] == 9).all()
+
+
 # ------------------------------------------------------------------ attention
 
 @pytest.mark.parametrize("G", range(1, 9))
@@ -126,6 +152,18 @@ def test_long_lists_and_long_chunks(C):
     for ids in (_all(c), [[np.arange(0, 5000, 2)], [np.array([0, 2])]], [[np.arange(2040, 2060)], [np.array([1])]]):
         out, lse = c.attend(qb, ids)
         c.check(qb, ids, out, lse)
+
+
+def test_more_pairs_than_workgroups(C):
+    """528 (sequence, head) pairs: one split each, which nobody merges."""
+    r = np.random.default_rng(15)
+    lens = [int(x) for x in r.integers(1, 400, size=66)]
+    c = C.Cache(34, 8, 2, lens, [C.cut(r, n, 3, 30) for n in lens])
+    qb, ids = c.query(), c.lists(0.8)
+    out, lse = c.attend(qb, ids)
+    for b in (0, 17, 65):
+        for h in range(8):
+            C.check_attention(c.heads(qb, b, h), c.k4(b, h), c.v4(b, h), c4.active_rows(c.bounds[b], c.lens[b], ids[b][h]), out[b, 2 * h:2 * h + 2], lse[b, 2 * h:2 * h + 2], (b, h))
 
 
 def test_a_list_of_more_passes_than_slots(C):
