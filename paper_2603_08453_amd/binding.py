@@ -482,7 +482,7 @@ def _move4(call, where, K, V, K4, V4, first, counts, stream, store):
         return
     B, H_kv, rows, d = K.shape
     assert K.shape == V.shape and K.stride() == V.stride() and K4.shape == V4.shape and K4.stride() == V4.stride()
-    assert K4.shape[:2] == K.shape[:2] and K.element_size() == 2
+    assert K4.shape[:2] == K.shape[:2] and K.element_size() == V.element_size() == 2 and V4.element_size() == 1
     counts = [rows] * B if counts is None else [int(n) for n in counts]
     first = None if first is None else [int(n) for n in first]
     assert len(counts) == B and max(counts, default=0) <= rows and (first is None or len(first) == B)
@@ -506,7 +506,7 @@ def lc_sparse_decode4(idx: Index, q, K4, V4, chunk_ids, counts, out, ws, lse=Non
     """lc_sparse_decode over a 4-bit cache (uint8 [B][H_kv][tokens][68])."""
     if _done((_fast_mod or _fast()).sparse_decode4(idx.address, q, K4, V4, chunk_ids, counts, out, ws, lse, stream), "lc_sparse_decode4"):
         return
-    assert K4.stride() == V4.stride()
+    assert K4.stride() == V4.stride() and V4.element_size() == 1
     _check(lib().lc_sparse_decode4(idx.handle, _ptr(q), _ptr(K4), _ptr(V4), _strides4(K4), _ptr(chunk_ids), _ptr(counts),
                                    chunk_ids.shape[2], q.shape[1], _ptr(out), _ptr(lse), _ptr(ws), ws.numel() * ws.element_size(),
                                    _stream(stream)), "lc_sparse_decode4")
@@ -519,7 +519,7 @@ def lc_append4(idx: Index, K4, V4, k_new, v_new, close_chunk: Optional[Sequence[
     cc = None
     if close_chunk is not None:
         cc = (ctypes.c_uint8 * len(close_chunk))(*[1 if c else 0 for c in close_chunk])
-    assert K4.stride() == V4.stride()
+    assert K4.stride() == V4.stride() and V4.element_size() == 1
     _check(lib().lc_append4(idx.handle, _ptr(K4), _ptr(V4), _strides4(K4), _ptr(k_new), _ptr(v_new), cc, _stream(stream)), "lc_append4")
 
 
@@ -555,7 +555,8 @@ def lc_evict_rows(idx: Index, keep_ids, keep_bounds, keep_counts, K, V, K_to, V_
     """The kept chunks' rows and the open tail's from K and V to the front of K_to and V_to; bf16 caches, or 4-bit ones (uint8)."""
     if _done((_fast_mod or _fast()).evict_rows(idx.address, keep_ids, keep_bounds, keep_counts, K, V, K_to, V_to, weights, weights_to, stream), "lc_evict_rows"):
         return
-    assert K.stride() == V.stride() and K_to.stride() == V_to.stride() and K.element_size() == K_to.element_size()
+    assert K.stride() == V.stride() and K_to.stride() == V_to.stride()
+    assert K.element_size() in (1, 2) and all(t.element_size() == K.element_size() for t in (V, K_to, V_to)), "caches must be all bfloat16 or all of 4 bits"
     call, strides = (lib().lc_evict_rows4, _strides4) if K.element_size() == 1 else (lib().lc_evict_rows, _strides3)
     _check(call(idx.handle, _ptr(keep_ids), _ptr(keep_bounds), _ptr(keep_counts), _ptr(K), _ptr(V), strides(K), _ptr(K_to), _ptr(V_to),
                 strides(K_to), _ptr(weights), _ptr(weights_to), _stream(stream)), "lc_evict_rows")

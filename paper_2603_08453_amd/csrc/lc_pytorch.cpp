@@ -289,7 +289,7 @@ bool cache4_strides(const at::Tensor& K4, const at::Tensor& V4, int64_t (&s)[3])
         PyErr_SetString(PyExc_AssertionError, "K4 and V4 must have the same strides");
         return false;
     }
-    if (K4.dim() != 4 || K4.size(3) != LC_CACHE4_ROW || K4.stride(3) != 1 || K4.element_size() != 1) {
+    if (K4.dim() != 4 || K4.size(3) != LC_CACHE4_ROW || K4.stride(3) != 1 || K4.element_size() != 1 || V4.element_size() != 1) {
         PyErr_SetString(PyExc_AssertionError, "4-bit cache must be uint8 [B][H_kv][tokens][68] with a row's bytes contiguous");
         return false;
     }
@@ -321,7 +321,7 @@ PyObject* move4(PyObject*, PyObject* const* args, Py_ssize_t n) {
         const bool store = a[0] == Py_True;
         const at::Tensor *K = a.tensor(1), *V = a.tensor(2), *K4 = a.tensor(3), *V4 = a.tensor(4);
         if (!K || !V || !K4 || !V4 || a.foreign()) return false;
-        if (K->dim() != 4 || K4->dim() != 4 || K->element_size() != 2 || !K->sizes().equals(V->sizes()) || !K4->sizes().equals(V4->sizes()) ||
+        if (K->dim() != 4 || K4->dim() != 4 || K->element_size() != 2 || V->element_size() != 2 || !K->sizes().equals(V->sizes()) || !K4->sizes().equals(V4->sizes()) ||
             K->size(0) != K4->size(0) || K->size(1) != K4->size(1) || K->size(0) > 256 || K->size(2) > 0x7fffffffL || K4->size(2) > 0x7fffffffL)
             return false;
         int64_t s[3], s4[3];
@@ -463,7 +463,8 @@ PyObject* evict_rows(PyObject*, PyObject* const* args, Py_ssize_t n) {
         if (!K || !V || !K_to || !V_to || a.foreign()) return false;
         const bool in4 = K->element_size() == 1;
         int64_t s[3], st_to[3];
-        if (K->element_size() != K_to->element_size()) return false;
+        for (const at::Tensor* t : {K, V, K_to, V_to})
+            if (t->element_size() != (in4 ? 1 : 2)) return false;
         if (in4 ? !cache4_strides(*K, *V, s) || !cache4_strides(*K_to, *V_to, st_to) : !cache_strides(*K, *V, false, s) || !cache_strides(*K_to, *V_to, false, st_to))
             return true;
         const int32_t* const ids = static_cast<const int32_t*>(a.ptr(1));

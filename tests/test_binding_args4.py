@@ -132,6 +132,24 @@ def test_eviction(seen, t):
         lc.lc_evict_rows(Index, t["keep"], t["bounds"], t["n"], t["K"], t["V"], t["K4b"], t["V4b"], stream=Stream)
 
 
+def test_halves_of_a_cache_with_other_types(seen, t):
+    """Shapes and strides alike, a smaller or larger element: rows would be read behind the tensor's end."""
+    bytes_, floats = torch.zeros(B, H, T, 128, dtype=torch.uint8), torch.zeros(B, H, T, 128)
+    shorts = torch.zeros(B, H, T + 1, 72, dtype=torch.int16)[..., 2:70]
+    keep = (t["keep"], t["bounds"], t["n"])
+    for call in (lambda: lc.lc_cache4_store(t["K"], bytes_, t["K4"], t["V4"], stream=Stream),
+                 lambda: lc.lc_cache4_load(t["K4"], shorts, t["K"], t["V"], stream=Stream),
+                 lambda: lc.lc_sparse_decode4(Index, t["q"], t["K4"], shorts, t["ids"], t["counts"], t["out"], t["ws"], stream=Stream),
+                 lambda: lc.lc_append4(Index, t["K4"], shorts, t["row"], t["row"], stream=Stream),
+                 lambda: lc.lc_evict_rows(Index, *keep, t["K"], bytes_, t["Kb"], t["Vb"], stream=Stream),
+                 lambda: lc.lc_evict_rows(Index, *keep, t["K"], t["V"], t["Kb"], bytes_, stream=Stream),
+                 lambda: lc.lc_evict_rows(Index, *keep, floats, floats, floats, floats, stream=Stream),
+                 lambda: lc.lc_evict_rows(Index, *keep, t["K4"], t["V4"], t["K4b"], shorts, stream=Stream)):
+        with pytest.raises(AssertionError):
+            call()
+    assert seen == []
+
+
 def test_other_threads_run_while_the_library_works(t):
     """The entry points replaced by the C library's usleep, whose argument is the handle: 200 ms in which another thread has to get on."""
     import threading
