@@ -56,7 +56,7 @@ lc_weigh_kernel(const LcWeighArgs a) {
     const __amdgpu_buffer_rsrc_t ids_r = lc_buffer(a.ids + (size_t)bh * a.cap, (int)(min((long long)a.cap, 1LL << 28) * 4));
     const int guess = part * LC_WG_WAVES;
     int id = lc_buf_load_i32(ids_r, guess + lane), before = lc_buf_load_i32(ids_r, max(0, guess + lane - 1));
-    const int count = max(0, min(a.counts[bh], a.cap)), M = ix.state[bh * 4 + 1];
+    const int count = max(0, min(a.counts[bh], min(a.cap, 1 << 28))), M = ix.state[bh * 4 + 1];
     const int per = max(LC_WG_WAVES, (count + parts - 1) / parts);
     const int e_lo = part * per, e_hi = min(count, e_lo + per);
     if (e_lo >= e_hi) return;
@@ -198,7 +198,7 @@ lc_weigh_kernel(const LcWeighArgs a) {
 
 template <bool IN4>
 int launch_weigh(LcWeighArgs& a, hipStream_t stream) {
-    const int pairs = a.ix.B * a.ix.H, all = (a.cap + LC_WG_WAVES - 1) / LC_WG_WAVES, fit = (LC_WG_GROUPS + pairs - 1) / pairs;
+    const int pairs = a.ix.B * a.ix.H, all = (a.cap - 1) / LC_WG_WAVES + 1, fit = (LC_WG_GROUPS + pairs - 1) / pairs;
     hipLaunchKernelGGL((lc_weigh_kernel<IN4>), dim3(a.ix.H, a.ix.B, all < fit ? all : fit), dim3(LC_WG_THREADS), 0, stream, a);
     LC_HIP_CHECK(hipGetLastError());
     return LC_OK;

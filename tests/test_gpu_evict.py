@@ -120,6 +120,22 @@ def test_weights_of_lists_longer_than_the_workgroups(C, bits):
         assert np.all(np.abs(got[b, h] - want) <= (math.expm1(x) + 16 * C.EPS) * (want - before[b, h]) + 2 * C.EPS * want), (b, h)
 
 
+@pytest.mark.parametrize("bits", [16, 4])
+def test_a_table_with_the_largest_room(C, bits):
+    """cap = 2^31 - 1, the lists as short as any."""
+    import torch
+    c = C.Cache(54, 1, 2, [300], [C.cut(np.random.default_rng(54), 300, 2, 20)])
+    keys = c.k4 if bits == 4 else (lambda b, h: wl.bf16_bits_to_f64(c.kb[b][h]))
+    qb, ids = c.query(), c.lists(0.7)
+    t, n = c.table(ids)
+    large = torch.empty(1, 1, 2**31 - 1, dtype=torch.int32, device="cuda")
+    large[:, :, :t.shape[2]] = t
+    lse = _lse(C, c, qb, ids, keys)
+    before = np.zeros((1, 1, c.cfg.max_chunks), dtype=np.float32)
+    got = _weigh(C, c, qb, ids, lse, before, bits, table=(large, n))
+    _check_weights(C, c, qb, ids, lse, before, got, keys)
+
+
 def test_entries_and_heads_that_add_nothing(C):
     import torch
     c = C.Cache(51, 1, 3, [200], [np.arange(0, 201, 10)])
