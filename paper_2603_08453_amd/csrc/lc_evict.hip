@@ -206,12 +206,14 @@ int launch_weigh(LcWeighArgs& a, hipStream_t stream) {
 
 // ---------------------------------------------------------------- whom to keep
 #define LC_EV_THREADS 1024
+#define LC_EV_SUM 256             // chunks of a workgroup that sums weights
 #define LC_EV_DIGIT 11
 #define LC_EV_BINS (1 << LC_EV_DIGIT)
 #define LC_EV_FEW 64              // chunks among which the cut is found by comparing each with each
 #define LC_EV_FUSED_MAX 4096      // chunks up to which the selecting workgroup sums the weights itself
 
-// Order-preserving map of a double: larger weight, larger key; what is not a number comes last (key 0).
+// Order-preserving map of a double: larger weight, larger key; what is not a number comes last (key 0).  Pinned chunks have a key behind all of them.
+#define LC_EV_PINNED 0xffffffffffffffffull
 __device__ __forceinline__ unsigned long long lc_weight_key(double w) {
     if (!(w == w)) return 0ull;
     const unsigned long long u = (unsigned long long)__double_as_longlong(w + 0.0);
@@ -232,19 +234,13 @@ __device__ __forceinline__ double lc_chunk_weight(const float* w, int H, int cap
     return sum;
 }
 
-__global__ void __launch_bounds__(256)
-lc_evict_keys_kernel(LcDev ix, const float* weights, unsigned long long* keys) {
-    const int b = blockIdx.y, M = min(ix.state[b * ix.H * 4 + 1], ix.cap[0]);
-    for (int j = blockIdx.x * 256 + threadIdx.x; j < M; j += gridDim.x * 256)
-        keys[(size_t)b * ix.cap[0] + j] = lc_weight_key(lc_chunk_weight(weights + (size_t)b * ix.H * ix.cap[0] + j, ix.H, ix.cap[0]));
-}
-
 struct LcEvictArgs {
     LcDev ix;
     const float* weights;
-    const unsigned long long* keys;
+    unsigned long long* keys;
     int32_t *ids, *bounds, *counts, *lens;
     int keep, recent, sink;
+    int sums;             // workgroups of a sequence that have summed the weights
 };
 
 // Minimum or maximum over the wavefront, in lane 63 (DPP shifts; lanes without a source keep their own).
@@ -260,15 +256,55 @@ __device__ __forceinline__ uint32_t lc_wave_extreme(uint32_t v) {
     return v;
 }
 
+// Keys of many chunks, by many workgroups.  Each leaves the tokens of its chunks that may be kept or not, and the smallest and the largest upper half of their keys, in
+// the list of ids, which has more room than that and is written behind all else.
+__global__ void __launch_bounds__(LC_EV_SUM)
+lc_evict_keys_kernel(const LcEvictArgs a) {
+    lc_fetch_args<sizeof(LcEvictArgs)>();
+    __shared__ uint32_t red_sh[3][LC_EV_SUM / 64];
+    const LcDev& ix = a.ix;
+    const int b = blockIdx.y, tid = threadIdx.x, M = min(ix.state[b * ix.H * 4 + 1], ix.cap[0]);
+    const int* bnd = ix.bounds + (size_t)b * (ix.cap[0] + 1);
+    const int last = bnd[M];
+    int tok = 0;
+    uint32_t lo = 0xffffffffu, hi = 0u;
+    for (int j = blockIdx.x * LC_EV_SUM + tid; j < M; j += gridDim.x * LC_EV_SUM) {
+        const int begin = bnd[j], end = bnd[j + 1];
+        unsigned long long k = lc_weight_key(lc_chunk_weight(a.weights + (size_t)b * ix.H * ix.cap[0] + j, ix.H, ix.cap[0]));
+        if (begin < a.sink || end > last - a.recent) {
+            k = LC_EV_PINNED;
+        } else {
+            tok += end - begin;
+            lo = min(lo, (uint32_t)(k >> 32));
+            hi = max(hi, (uint32_t)(k >> 32));
+        }
+        a.keys[(size_t)b * ix.cap[0] + j] = k;
+    }
+    lo = lc_wave_extreme<false>(lo);
+    hi = lc_wave_extreme<true>(hi);
+    tok = lc_wave_scan_incl(tok);
+    if ((tid & 63) == 63) { red_sh[0][tid >> 6] = lo; red_sh[1][tid >> 6] = hi; red_sh[2][tid >> 6] = (uint32_t)tok; }
+    __syncthreads();
+    if (tid == 0) {
+        int32_t* const out = a.ids + (size_t)b * ix.cap[0] + 3 * blockIdx.x;
+        lo = min(min(red_sh[0][0], red_sh[0][1]), min(red_sh[0][2], red_sh[0][3]));
+        hi = max(max(red_sh[1][0], red_sh[1][1]), max(red_sh[1][2], red_sh[1][3]));
+        out[0] = (int32_t)lo;
+        out[1] = (int32_t)hi;
+        out[2] = (int32_t)((red_sh[2][0] + red_sh[2][1]) + (red_sh[2][2] + red_sh[2][3]));
+    }
+}
+
 // One workgroup per sequence: the pinned chunks, and of the others the longest prefix by (key descending, id ascending) that fits.  The cut
 // is found digit by digit of the keys' distance from the smallest: tokens per digit, then the digit at which their sum from above no longer fits,
 // until few chunks are left at the cut (mostly after one digit) or all their keys are equal.  (Digits of the keys themselves begin with the
 // exponent, whose few values put all LDS atomics on a few words.)
 // A thread keeps C chunks, 1024 apart, in registers; chunks beyond (more than 12288, or an index that has grown since the launch was captured) are read where they are
 // each time.
-// What bounds it is a chain of barriers, LDS atomics and the first loads in one compute unit per sequence: 113 chunks 6.0 us, 4 sequences of 455 6.1, 10.9 K chunks 16.9 with the
-// weights' sums before it (4.5; up to 4096 chunks the selecting workgroup makes them, which saves a launch), 26 K chunks 41, 87 K chunks 176.
-// (Digits of the keys from the first bit in which they differ, ranks by a single wavefront and scans of 1024 chunks at a time: 9, 39 and 44 us for the first three.)
+// What bounds it is a chain of barriers, LDS atomics and the first loads in one compute unit per sequence: 113 chunks 6.0 us, 4 sequences of 455 6.1, 10.9 K chunks 16.4 with the
+// weights' sums before it (4.5; up to 4096 chunks the selecting workgroup makes them, which saves a launch), 4 sequences of 12 K 17.7, 26 K chunks 44, 87 K chunks 145.  (With the pinned
+// chunks in masks beside the keys, and the range of the keys found here instead of with the sums, the last four took 16.9, 18.2, 52 and 177; digits of the keys from the first
+// bit in which they differ, ranks by a single wavefront and scans of 1024 chunks at a time: the first three 9, 39 and 44.)
 template <int C, bool FUSED>
 __global__ void __launch_bounds__(LC_EV_THREADS)
 lc_evict_select_kernel(const LcEvictArgs a) {
@@ -286,73 +322,83 @@ lc_evict_select_kernel(const LcEvictArgs a) {
     const int* bnd = ix.bounds + (size_t)b * (ix.cap[0] + 1);
     const unsigned long long* keys = a.keys + (size_t)b * ix.cap[0];
     const float* weights = a.weights + (size_t)b * ix.H * ix.cap[0];
+    int32_t* ids = a.ids + (size_t)b * ix.cap[0];
     const int last = bnd[M];
-    auto key_of = [&](int j) LC_INLINE { return FUSED ? lc_weight_key(lc_chunk_weight(weights + j, ix.H, ix.cap[0])) : keys[j]; };
-    auto pinned = [&](int begin, int end) LC_INLINE { return begin < a.sink || end > last - a.recent; };
+    auto key_of = [&](int j, int begin, int end) LC_INLINE -> unsigned long long {
+        if constexpr (!FUSED) return keys[j];
+        const unsigned long long k = lc_weight_key(lc_chunk_weight(weights + j, ix.H, ix.cap[0]));
+        return begin < a.sink || end > last - a.recent ? LC_EV_PINNED : k;
+    };
 
     unsigned long long key[C];
     int len[C];
-    uint32_t pins = 0u, live = 0u;                           // bit c: this thread's chunk c is pinned, may be kept or not
     {
-        int end[C];
         // (no branch around a load: they are on their way together)
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            const int j = max(0, min(tid + c * NT, M - 1));
-            len[c] = bnd[j];
-            end[c] = bnd[j + 1];
-            key[c] = key_of(j);
-        }
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const uint32_t real = tid + c * NT < M ? 1u : 0u, pin = pinned(len[c], end[c]) ? 1u : 0u;
-            pins |= (real & pin) << c;
-            live |= (real & ~pin) << c;
-            len[c] = end[c] - len[c];
+            const int j = max(0, min(tid + c * NT, M - 1)), begin = bnd[j], end = bnd[j + 1];
+            const bool real = tid + c * NT < M;
+            const unsigned long long k = key_of(j, begin, end);
+            key[c] = real ? k : LC_EV_PINNED;
+            len[c] = real ? end - begin : 0;
         }
     }
-    // f(whether it may be kept or not, chunk, its tokens, its key) of the chunks in registers, then of the others
+    // f(chunk, its tokens, its key) of the chunks in registers, then of the others
     auto each = [&](auto f) LC_INLINE {
 #pragma unroll
         for (int c = 0; c < C; ++c)
-            if (c * NT < M) f((live >> c) & 1u, tid + c * NT, len[c], key[c]);
+            if (c * NT < M) f(tid + c * NT, len[c], key[c]);
         // (four at a time, their loads together)
         for (int j0 = C * NT + tid; j0 < M; j0 += 4 * NT) {
-            int begin[4], end[4];
+            int n[4];
             unsigned long long k[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const int j = min(j0 + u * NT, M - 1);
-                begin[u] = bnd[j];
-                end[u] = bnd[j + 1];
-                k[u] = key_of(j);
+                const int j = min(j0 + u * NT, M - 1), begin = bnd[j], end = bnd[j + 1];
+                n[u] = end - begin;
+                k[u] = key_of(j, begin, end);
             }
 #pragma unroll
             for (int u = 0; u < 4; ++u)
-                if (j0 + u * NT < M && !pinned(begin[u], end[u])) f(1u, j0 + u * NT, end[u] - begin[u], k[u]);
+                if (j0 + u * NT < M) f(j0 + u * NT, n[u], k[u]);
         }
     };
 
-    // tokens of those, the smallest and the largest of their keys (of the upper halves)
+    // tokens of those that are not pinned, the smallest and the largest of their keys (of the upper halves)
     int tok = 0;
     uint32_t lo = 0xffffffffu, hi = 0u;
-    each([&](uint32_t is, int, int n, unsigned long long k) LC_INLINE {
-        const uint32_t none = is - 1u, top = (uint32_t)(k >> 32);    // (all ones where it is not)
-        tok += n & ~(int)none;
-        lo = min(lo, top | none);
-        hi = max(hi, top & ~none);
-    });
+    if constexpr (FUSED) {
+        each([&](int, int n, unsigned long long k) LC_INLINE {
+            const bool is = k != LC_EV_PINNED;
+            tok += is ? n : 0;
+            lo = min(lo, (uint32_t)(k >> 32));               // (a pinned one's: the largest there is)
+            hi = max(hi, is ? (uint32_t)(k >> 32) : 0u);
+        });
+    } else {
+        for (int i = lane; i < a.sums; i += 64) {            // (every wavefront all of them)
+            lo = min(lo, (uint32_t)ids[3 * i]);
+            hi = max(hi, (uint32_t)ids[3 * i + 1]);
+            tok += ids[3 * i + 2];
+        }
+    }
     for (int i = tid; i < LC_EV_BINS; i += NT) tok_sh[i] = 0;
     if (tid < LC_EV_FEW) sum_sh[tid] = 0;
     if (tid == 0) { few_sh = 0; last_key_sh = 0ull; last_id_sh = -1; }
     lo = lc_wave_extreme<false>(lo);
     hi = lc_wave_extreme<true>(hi);
     tok = lc_wave_scan_incl(tok);
-    if (lane == 63) { red_sh[wave] = lo; red_sh[NW + wave] = hi; red_sh[2 * NW + wave] = (uint32_t)tok; }
-    __syncthreads();
-    lo = (uint32_t)lc_readlane((int)lc_wave_extreme<false>(red_sh[lane & (NW - 1)]), 63);
-    hi = (uint32_t)lc_readlane((int)lc_wave_extreme<true>(red_sh[NW + (lane & (NW - 1))]), 63);
-    const int others = lc_readlane(lc_wave_scan_incl(lane < NW ? (int)red_sh[2 * NW + lane] : 0), 63);
+    if constexpr (FUSED) {
+        if (lane == 63) { red_sh[wave] = lo; red_sh[NW + wave] = hi; red_sh[2 * NW + wave] = (uint32_t)tok; }
+        __syncthreads();
+        lo = lc_wave_extreme<false>(red_sh[lane & (NW - 1)]);
+        hi = lc_wave_extreme<true>(red_sh[NW + (lane & (NW - 1))]);
+        tok = lc_wave_scan_incl(lane < NW ? (int)red_sh[2 * NW + lane] : 0);
+    } else {
+        __syncthreads();                                     // (the counts above are zero)
+    }
+    lo = (uint32_t)lc_readlane((int)lo, 63);
+    hi = (uint32_t)lc_readlane((int)hi, 63);
+    const int others = lc_readlane(tok, 63);
     int left = max(0, a.keep - (last - others));             // tokens for the others, behind the pinned ones
 
     // Keys of [base, base + 2^shift) are at the cut: of those the first `left` tokens' worth is kept, of larger ones all, of smaller ones none.
@@ -363,8 +409,8 @@ lc_evict_select_kernel(const LcEvictArgs a) {
     bool few = false;
     while (!all && shift > 0 && !few) {
         const int next = max(0, shift - LC_EV_DIGIT);
-        each([&](uint32_t is, int, int n, unsigned long long k) LC_INLINE {
-            if (is && at_cut(k)) atomicAdd(&tok_sh[(int)((k - base) >> next)], n);
+        each([&](int, int n, unsigned long long k) LC_INLINE {
+            if (k != LC_EV_PINNED && at_cut(k)) atomicAdd(&tok_sh[(int)((k - base) >> next)], n);
         });
         __syncthreads();
         // from the largest digit down: thread t has digits (BINS - 1 - 2 t) and the one below
@@ -379,8 +425,8 @@ lc_evict_select_kernel(const LcEvictArgs a) {
         left -= found_sh[1];
         shift = next;
         // the chunks at the cut, if they are few
-        each([&](uint32_t is, int j, int n, unsigned long long k) LC_INLINE {
-            if (is && at_cut(k)) {
+        each([&](int j, int n, unsigned long long k) LC_INLINE {
+            if (k != LC_EV_PINNED && at_cut(k)) {
                 const int i = atomicAdd(&few_sh, 1);
                 if (i < LC_EV_FEW) {
                     key_sh[i] = k;
@@ -431,7 +477,7 @@ lc_evict_select_kernel(const LcEvictArgs a) {
             int n = 0;
             if (j < M) {
                 const int begin = bnd[j], end = bnd[j + 1];
-                if (!pinned(begin, end) && key_of(j) == base) n = end - begin;
+                if (key_of(j, begin, end) == base) n = end - begin;
             }
             int total;
             const int before = lc_block_scan<NT>(n, scan_sh, &total);
@@ -443,21 +489,21 @@ lc_evict_select_kernel(const LcEvictArgs a) {
     __syncthreads();
     const unsigned long long last_key = all ? 0ull : last_key_sh;
     const int last_id = all ? 0x7fffffff : last_id_sh;
-    auto keeps = [&](unsigned long long k, int j) LC_INLINE { return k > last_key || (k == last_key && j <= last_id); };
+    auto keeps = [&](unsigned long long k, int j) LC_INLINE { return k > last_key || (k == last_key && j <= last_id); };   // (pinned ones too)
 
     // ids, boundaries, the rest of both lists
-    int32_t* ids = a.ids + (size_t)b * ix.cap[0];
     int32_t* bounds = a.bounds + (size_t)b * (ix.cap[0] + 1);
     int n_keep = 0, n_tok = 0;
     {
         // the chunks in registers all at once: wavefronts' counts and tokens, then each its place
+        uint32_t kept = 0u;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int j = tid + c * NT;
             int count = 0, tokens = 0;
             if (c * NT < M) {
-                const bool k = ((pins | (keeps(key[c], j) ? live : 0u)) >> c) & 1u;
-                pins = k ? pins | (1u << c) : pins;          // (from here on: kept)
+                const bool k = j < M && keeps(key[c], j);
+                kept |= k ? 1u << c : 0u;
                 const int n = k ? len[c] : 0;
                 tokens = lc_wave_scan_incl(n);
                 len[c] = tokens - n;                         // (from here on: tokens kept before it, of the wavefront)
@@ -483,7 +529,7 @@ lc_evict_select_kernel(const LcEvictArgs a) {
 #pragma unroll
         for (int c = 0; c < C; ++c)
             if (c * NT < M) {
-                const bool k = (pins >> c) & 1u;
+                const bool k = (kept >> c) & 1u;
                 const int i = slab_cnt[c * NW + wave] + __popcll(__ballot(k) & ((1ull << lane) - 1ull));
                 if (k) {
                     ids[i] = tid + c * NT;
@@ -501,12 +547,12 @@ lc_evict_select_kernel(const LcEvictArgs a) {
 #pragma unroll
         for (int u = 0; u < 5; ++u) edge[u] = bnd[min(j + u, M)];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) k[u] = all ? 0ull : key_of(min(j + u, M - 1));
+        for (int u = 0; u < 4; ++u) k[u] = all ? 0ull : key_of(min(j + u, M - 1), edge[u], edge[u + 1]);
         uint32_t kept = 0u;
         int n = 0;
 #pragma unroll
         for (int u = 0; u < 4; ++u)
-            if (j + u < M && (pinned(edge[u], edge[u + 1]) || keeps(k[u], j + u))) {
+            if (j + u < M && keeps(k[u], j + u)) {
                 kept |= 1u << u;
                 n += edge[u + 1] - edge[u];
             }
@@ -772,12 +818,13 @@ int lc_evict_select(const lc_index* idx, const float* weights, int keep_tokens, 
     a.keys = keys;
     a.ids = keep_ids; a.bounds = keep_bounds; a.counts = keep_counts; a.lens = keep_lens;
     a.keep = keep_tokens; a.recent = recent_tokens; a.sink = idx->cfg.sink_tokens;
+    a.sums = (most + LC_EV_SUM - 1) / LC_EV_SUM;
     const dim3 grid(idx->B), block(LC_EV_THREADS);
     if (most <= LC_EV_FUSED_MAX) {
         if (most <= LC_EV_THREADS) hipLaunchKernelGGL((lc_evict_select_kernel<1, true>), grid, block, 0, st, a);
         else hipLaunchKernelGGL((lc_evict_select_kernel<4, true>), grid, block, 0, st, a);
     } else {
-        hipLaunchKernelGGL(lc_evict_keys_kernel, dim3((most + 255) / 256, idx->B), dim3(256), 0, st, idx->dev, weights, keys);
+        hipLaunchKernelGGL(lc_evict_keys_kernel, dim3(a.sums, idx->B), dim3(LC_EV_SUM), 0, st, a);
         LC_HIP_CHECK(hipGetLastError());
         hipLaunchKernelGGL((lc_evict_select_kernel<12, false>), grid, block, 0, st, a);
     }
