@@ -396,7 +396,7 @@ int lc_weigh_chunks4(const lc_index* idx, const void* q, const void* K4, const i
  *   keep_bounds  int32 [B][max_chunks + 1] out: where the kept chunks begin in the new cache; from keep_counts[b] on the end of the last
  *   keep_counts  int32 [B] out
  *   keep_lens    int32 [B] out or NULL: tokens of the new cache, the open tail's among them
- *   ws           any workspace of lc_decode_workspace_bytes() (B * max_chunks * 8 bytes are used)
+ *   ws           any workspace of lc_decode_workspace_bytes() (B * max_chunks * 8 bytes are used, with more than 14336 max_chunks 16)
  */
 int lc_evict_select(const lc_index* idx, const float* weights, int keep_tokens, int recent_tokens, int32_t* keep_ids, int32_t* keep_bounds,
                     int32_t* keep_counts, int32_t* keep_lens, void* ws, size_t ws_bytes, void* stream);

@@ -207,10 +207,13 @@ int launch_weigh(LcWeighArgs& a, hipStream_t stream) {
 // ---------------------------------------------------------------- whom to keep
 #define LC_EV_THREADS 1024
 #define LC_EV_SUM 256             // chunks of a workgroup that sums weights
+#define LC_EV_SLAB 4096           // chunks a workgroup takes at a time where several share a sequence
+#define LC_EV_GROUPS 128          // of those workgroups at most
 #define LC_EV_DIGIT 11
 #define LC_EV_BINS (1 << LC_EV_DIGIT)
 #define LC_EV_FEW 64              // chunks among which the cut is found by comparing each with each
-#define LC_EV_FUSED_MAX 4096      // chunks up to which the selecting workgroup sums the weights itself
+#define LC_EV_FUSED_MAX 4096      // chunks up to which the selecting workgroup sums the weights itself (8192 of 8 heads: 14.1 us, summed by others 15.3; of 32: 21.1, 15.8)
+#define LC_EV_SINGLE_MAX 14336    // chunks up to which a sequence has one workgroup (12288: 16.1 us, with several 21.3; 14000: 19.2, 22.4; 16384: 24.4, 21.6; 26 K: 43, 24)
 
 // Order-preserving map of a double: larger weight, larger key; what is not a number comes last (key 0).  Pinned chunks have a key behind all of them.
 #define LC_EV_PINNED 0xffffffffffffffffull
@@ -241,7 +244,12 @@ struct LcEvictArgs {
     int32_t *ids, *bounds, *counts, *lens;
     int keep, recent, sink;
     int sums;             // workgroups of a sequence that have summed the weights
+    int32_t* range;       // what they leave, sequences range_seq apart
+    long long range_seq;
+    int32_t* spare;       // where several workgroups share a sequence: 2 max_chunks for each
 };
+// spare: the digits' tokens, the cut, its chunks' number, the last that is kept, {chunks, tokens} that each workgroup keeps, the ranges of the keys, the chunks at the cut
+enum { LC_EVS_CUT = LC_EV_BINS, LC_EVS_N = LC_EVS_CUT + 4, LC_EVS_LAST, LC_EVS_KEPT = LC_EVS_LAST + 3, LC_EVS_RANGE = LC_EVS_KEPT + 2 * LC_EV_GROUPS };
 
 // Minimum or maximum over the wavefront, in lane 63 (DPP shifts; lanes without a source keep their own).
 template <bool MAX>
@@ -256,8 +264,7 @@ __device__ __forceinline__ uint32_t lc_wave_extreme(uint32_t v) {
     return v;
 }
 
-// Keys of many chunks, by many workgroups.  Each leaves the tokens of its chunks that may be kept or not, and the smallest and the largest upper half of their keys, in
-// the list of ids, which has more room than that and is written behind all else.
+// Keys of many chunks, by many workgroups.  Each leaves the tokens of its chunks that are not pinned, and the smallest and the largest upper half of their keys.
 __global__ void __launch_bounds__(LC_EV_SUM)
 lc_evict_keys_kernel(const LcEvictArgs a) {
     lc_fetch_args<sizeof(LcEvictArgs)>();
@@ -266,6 +273,11 @@ lc_evict_keys_kernel(const LcEvictArgs a) {
     const int b = blockIdx.y, tid = threadIdx.x, M = min(ix.state[b * ix.H * 4 + 1], ix.cap[0]);
     const int* bnd = ix.bounds + (size_t)b * (ix.cap[0] + 1);
     const int last = bnd[M];
+    if (a.spare) {
+        int32_t* spare = a.spare + (size_t)b * 2 * ix.cap[0];
+        for (int i = blockIdx.x * LC_EV_SUM + tid; i < LC_EV_BINS; i += gridDim.x * LC_EV_SUM) spare[i] = 0;
+        if (blockIdx.x == 0 && tid == 0) spare[LC_EVS_N] = 0;
+    }
     int tok = 0;
     uint32_t lo = 0xffffffffu, hi = 0u;
     for (int j = blockIdx.x * LC_EV_SUM + tid; j < M; j += gridDim.x * LC_EV_SUM) {
@@ -286,12 +298,169 @@ lc_evict_keys_kernel(const LcEvictArgs a) {
     if ((tid & 63) == 63) { red_sh[0][tid >> 6] = lo; red_sh[1][tid >> 6] = hi; red_sh[2][tid >> 6] = (uint32_t)tok; }
     __syncthreads();
     if (tid == 0) {
-        int32_t* const out = a.ids + (size_t)b * ix.cap[0] + 3 * blockIdx.x;
+        int32_t* const out = a.range + b * a.range_seq + 3 * blockIdx.x;
         lo = min(min(red_sh[0][0], red_sh[0][1]), min(red_sh[0][2], red_sh[0][3]));
         hi = max(max(red_sh[1][0], red_sh[1][1]), max(red_sh[1][2], red_sh[1][3]));
         out[0] = (int32_t)lo;
         out[1] = (int32_t)hi;
         out[2] = (int32_t)((red_sh[2][0] + red_sh[2][1]) + (red_sh[2][2] + red_sh[2][3]));
+    }
+}
+
+// A lane's part of what the workgroups of the keys have left.
+__device__ __forceinline__ void lc_evict_range(const LcEvictArgs& a, int b, uint32_t& lo, uint32_t& hi, int& tok) {
+    const int32_t* from = a.range + b * a.range_seq;
+    for (int i = threadIdx.x & 63; i < a.sums; i += 64) {
+        lo = min(lo, (uint32_t)from[3 * i]);
+        hi = max(hi, (uint32_t)from[3 * i + 1]);
+        tok += from[3 * i + 2];
+    }
+}
+
+// ---- finding the cut
+struct LcCutSh {
+    int tok[LC_EV_BINS];
+    unsigned long long key[LC_EV_FEW], last_key;
+    int id[LC_EV_FEW], len[LC_EV_FEW], sum[LC_EV_FEW];
+    int scan[2 * (LC_EV_THREADS / 64)], found[2], few, last_id;
+};
+// (a barrier must follow)
+__device__ __forceinline__ void lc_cut_prepare(LcCutSh& sh) {
+    for (int i = threadIdx.x; i < LC_EV_BINS; i += LC_EV_THREADS) sh.tok[i] = 0;
+    if (threadIdx.x < LC_EV_FEW) sh.sum[threadIdx.x] = 0;
+    if (threadIdx.x == 0) { sh.few = 0; sh.last_key = 0ull; sh.last_id = -1; }
+}
+// Keys of [base, base + 2^shift) are at the cut: of those the first `left` tokens' worth is kept, of larger ones all, of smaller ones none.
+struct LcCut {
+    unsigned long long base;
+    int shift, left;      // (a shift of 64: before the first digit)
+    __device__ __forceinline__ int next() const { return max(0, shift - LC_EV_DIGIT); }
+    __device__ __forceinline__ bool digit(unsigned long long k, int* d) const {      // whether a key is at the cut, and its next digit
+        const unsigned long long x = (k - base) >> next();
+        *d = (int)x;
+        return k != LC_EV_PINNED && x < 1ull << (shift - next());
+    }
+    __device__ __forceinline__ bool at(unsigned long long k) const { return k != LC_EV_PINNED && ((k - base) >> shift) == 0ull; }
+    __device__ __forceinline__ bool above(unsigned long long k) const { return k == LC_EV_PINNED || (k >= base && !at(k)); }
+};
+// All keys from the smallest to the largest upper half (lo > hi: there is none).
+__device__ __forceinline__ LcCut lc_cut_of(uint32_t lo, uint32_t hi, int left) {
+    return {(unsigned long long)lo << 32, 32 + (lo < hi ? 32 - __clz((int)(hi - lo)) : 0), left};
+}
+// One digit less at the cut: the one at which the tokens from above (t1: of digit BINS - 1 - 2 thread, t0: of the one below) no longer fit.
+__device__ __forceinline__ void lc_cut_digit(LcCutSh& sh, LcCut& cut, int t1, int t0, bool clear) {
+    const int d1 = LC_EV_BINS - 1 - 2 * threadIdx.x;
+    int total;
+    const int before = lc_block_scan<LC_EV_THREADS>(t1 + t0, sh.scan, &total);
+    if (before <= cut.left && before + t1 > cut.left) { sh.found[0] = d1; sh.found[1] = before; }
+    else if (before + t1 <= cut.left && before + t1 + t0 > cut.left) { sh.found[0] = d1 - 1; sh.found[1] = before + t1; }
+    if (clear) sh.tok[d1] = sh.tok[d1 - 1] = 0;
+    __syncthreads();
+    cut.base += (unsigned long long)sh.found[0] << cut.next();
+    cut.left -= sh.found[1];
+    cut.shift = cut.next();
+}
+// sh.last_key, sh.last_id: every chunk up to them in the order is kept.  each(f): f(chunk, tokens, key) of all chunks at the cut and perhaps others, sorted(j, &tokens):
+// the key of chunk j < M.  listed: there may be few of them at the cut already.  More tokens are at the cut than are left.
+template <typename Each, typename Sorted>
+__device__ __forceinline__ void lc_cut_search(LcCutSh& sh, LcCut cut, bool listed, int M, Each each, Sorted sorted) {
+    constexpr int NT = LC_EV_THREADS, NW = NT / 64;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    // the chunks at the cut, if they are few
+    auto collect = [&]() LC_INLINE -> bool {
+        each([&](int j, int n, unsigned long long k) LC_INLINE {
+            if (cut.at(k)) {
+                const int i = atomicAdd(&sh.few, 1);
+                if (i < LC_EV_FEW) {
+                    sh.key[i] = k;
+                    sh.id[i] = j;
+                    sh.len[i] = n;
+                }
+            }
+        });
+        __syncthreads();
+        if (sh.few <= LC_EV_FEW) return true;
+        __syncthreads();
+        if (tid == 0) sh.few = 0;
+        __syncthreads();
+        return false;
+    };
+    bool few = listed && collect();
+    while (cut.shift > 0 && !few) {
+        each([&](int, int n, unsigned long long k) LC_INLINE {
+            int d;
+            if (cut.digit(k, &d)) atomicAdd(&sh.tok[d], n);
+        });
+        __syncthreads();
+        const int d1 = LC_EV_BINS - 1 - 2 * tid, t1 = sh.tok[d1], t0 = sh.tok[d1 - 1];
+        lc_cut_digit(sh, cut, t1, t0, true);
+        few = collect();
+    }
+    if (__builtin_expect(few, 1)) {
+        // a lane has a chunk at the cut, each wavefront some of those to compare it with
+        const int n = sh.few;
+        const unsigned long long k = lane < n ? sh.key[lane] : 0ull;
+        const int id = lane < n ? sh.id[lane] : 0x7fffffff;
+        int part = 0;
+        for (int i = wave; i < n; i += NW) {
+            const unsigned long long ki = sh.key[i];
+            if (ki > k || (ki == k && sh.id[i] <= id)) part += sh.len[i];
+        }
+        if (lane < n && part != 0) atomicAdd(&sh.sum[lane], part);
+        __syncthreads();
+        if (wave == 0) {
+            // (the sums of those that fit grow along the order: the last of them has the largest)
+            const int sum = sh.sum[lane];
+            const uint32_t mine = lane < n && sum <= cut.left ? (uint32_t)sum + 1u : 0u;
+            const uint32_t most = (uint32_t)lc_readlane((int)lc_wave_extreme<true>(mine), 63);
+            if (most == 0u) {
+                if (lane == 0) sh.last_key = cut.base + ((1ull << cut.shift) - 1ull);    // none at the cut
+            } else if (mine == most) {
+                sh.last_key = k;
+                sh.last_id = id;
+            }
+        }
+    } else {
+        // equal keys at the cut: the first of them
+        int tied = 0;
+        for (int j0 = 0; j0 < M; j0 += NT) {
+            const int j = j0 + tid;
+            int n = 0;
+            if (j < M && sorted(j, &n) != cut.base) n = 0;
+            int total;
+            const int before = lc_block_scan<NT>(n, sh.scan, &total);
+            if (n > 0 && before <= cut.left - tied - n) atomicMax(&sh.last_id, j);
+            tied = min(tied + total, 1 << 30);
+        }
+        if (tid == 0) sh.last_key = cut.base;
+    }
+    __syncthreads();
+}
+
+// The kept ones of chunks [j, hi), from place n_keep and token n_tok on: a thread has four chunks in a row, a scan for LC_EV_SLAB of them.
+template <typename Kept>
+__device__ __forceinline__ void lc_evict_place(int j0, int hi, const int* bnd, int32_t* ids, int32_t* bounds, int* scan_sh, int& n_keep, int& n_tok, Kept keeps) {
+    for (; j0 < hi; j0 += LC_EV_SLAB) {
+        const int j = j0 + 4 * (int)threadIdx.x;
+        int edge[5];
+#pragma unroll
+        for (int u = 0; u < 5; ++u) edge[u] = bnd[min(j + u, hi)];
+        uint32_t kept = keeps(j, edge);
+        int n = 0;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) n += (kept >> u) & 1u ? edge[u + 1] - edge[u] : 0;
+        int at, to, count, tokens;
+        lc_block_scan2<LC_EV_THREADS>(__popc(kept), n, scan_sh, &at, &to, &count, &tokens);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if ((kept >> u) & 1u) {
+                ids[n_keep + at] = j + u;
+                bounds[n_keep + at] = n_tok + to;
+                at += 1;
+                to += edge[u + 1] - edge[u];
+            }
+        n_keep += count;
+        n_tok += tokens;
     }
 }
 
@@ -301,20 +470,17 @@ lc_evict_keys_kernel(const LcEvictArgs a) {
 // exponent, whose few values put all LDS atomics on a few words.)
 // A thread keeps C chunks, 1024 apart, in registers; chunks beyond (more than 12288, or an index that has grown since the launch was captured) are read where they are
 // each time.
-// What bounds it is a chain of barriers, LDS atomics and the first loads in one compute unit per sequence: 113 chunks 6.0 us, 4 sequences of 455 6.1, 10.9 K chunks 16.4 with the
-// weights' sums before it (4.5; up to 4096 chunks the selecting workgroup makes them, which saves a launch), 4 sequences of 12 K 17.7, 26 K chunks 44, 87 K chunks 145.  (With the pinned
-// chunks in masks beside the keys, and the range of the keys found here instead of with the sums, the last four took 16.9, 18.2, 52 and 177; digits of the keys from the first
-// bit in which they differ, ranks by a single wavefront and scans of 1024 chunks at a time: the first three 9, 39 and 44.)
+// What bounds it is a chain of barriers, LDS atomics and the first loads in one compute unit per sequence: 113 chunks 5.9 us, 4 sequences of 455 6.1, 4096 9.5, 10.9 K 15.7 with the
+// weights' sums before it (4.5; up to 4096 chunks the selecting workgroup makes them, which saves a launch), 4 sequences of 12 K 16.6.  (With the pinned chunks in masks beside the
+// keys, and the range of the keys found here instead of with the sums: 10.9 K 16.9; with the loops over chunks in memory between the others in the code: the first two 6.3 and 6.5.
+// Digits of the keys from the first bit in which they differ, ranks by a single wavefront and scans of 1024 chunks at a time: 9 us for the first.)
 template <int C, bool FUSED>
 __global__ void __launch_bounds__(LC_EV_THREADS)
 lc_evict_select_kernel(const LcEvictArgs a) {
     lc_fetch_args<sizeof(LcEvictArgs)>();
     constexpr int NT = LC_EV_THREADS, NW = NT / 64;
-    __shared__ int tok_sh[LC_EV_BINS];
-    __shared__ unsigned long long key_sh[LC_EV_FEW], last_key_sh;
+    __shared__ LcCutSh sh;
     __shared__ uint32_t red_sh[3 * NW];
-    __shared__ int id_sh[LC_EV_FEW], len_sh[LC_EV_FEW], sum_sh[LC_EV_FEW];
-    __shared__ int scan_sh[2 * NW], found_sh[2], few_sh, last_id_sh;
     __shared__ int slab_cnt[C * NW], slab_tok[C * NW];
     const LcDev& ix = a.ix;
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -347,20 +513,22 @@ lc_evict_select_kernel(const LcEvictArgs a) {
     auto each = [&](auto f) LC_INLINE {
 #pragma unroll
         for (int c = 0; c < C; ++c)
-            if (c * NT < M) f(tid + c * NT, len[c], key[c]);
+            f(tid + c * NT, len[c], key[c]);
         // (four at a time, their loads together)
-        for (int j0 = C * NT + tid; j0 < M; j0 += 4 * NT) {
-            int n[4];
-            unsigned long long k[4];
+        if (__builtin_expect(M > C * NT, 0)) {
+            for (int j0 = C * NT + tid; j0 < M; j0 += 4 * NT) {
+                int n[4];
+                unsigned long long k[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int j = min(j0 + u * NT, M - 1), begin = bnd[j], end = bnd[j + 1];
-                n[u] = end - begin;
-                k[u] = key_of(j, begin, end);
+                for (int u = 0; u < 4; ++u) {
+                    const int j = min(j0 + u * NT, M - 1), begin = bnd[j], end = bnd[j + 1];
+                    n[u] = end - begin;
+                    k[u] = key_of(j, begin, end);
+                }
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    if (j0 + u * NT < M) f(j0 + u * NT, n[u], k[u]);
             }
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-                if (j0 + u * NT < M) f(j0 + u * NT, n[u], k[u]);
         }
     };
 
@@ -375,15 +543,9 @@ lc_evict_select_kernel(const LcEvictArgs a) {
             hi = max(hi, is ? (uint32_t)(k >> 32) : 0u);
         });
     } else {
-        for (int i = lane; i < a.sums; i += 64) {            // (every wavefront all of them)
-            lo = min(lo, (uint32_t)ids[3 * i]);
-            hi = max(hi, (uint32_t)ids[3 * i + 1]);
-            tok += ids[3 * i + 2];
-        }
+        lc_evict_range(a, b, lo, hi, tok);
     }
-    for (int i = tid; i < LC_EV_BINS; i += NT) tok_sh[i] = 0;
-    if (tid < LC_EV_FEW) sum_sh[tid] = 0;
-    if (tid == 0) { few_sh = 0; last_key_sh = 0ull; last_id_sh = -1; }
+    lc_cut_prepare(sh);
     lo = lc_wave_extreme<false>(lo);
     hi = lc_wave_extreme<true>(hi);
     tok = lc_wave_scan_incl(tok);
@@ -399,96 +561,16 @@ lc_evict_select_kernel(const LcEvictArgs a) {
     lo = (uint32_t)lc_readlane((int)lo, 63);
     hi = (uint32_t)lc_readlane((int)hi, 63);
     const int others = lc_readlane(tok, 63);
-    int left = max(0, a.keep - (last - others));             // tokens for the others, behind the pinned ones
-
-    // Keys of [base, base + 2^shift) are at the cut: of those the first `left` tokens' worth is kept, of larger ones all, of smaller ones none.
+    const int left = max(0, a.keep - (last - others));       // tokens for the others, behind the pinned ones
     const bool all = others <= left;
-    unsigned long long base = (unsigned long long)lo << 32;
-    int shift = 32 + (lo < hi ? 32 - __clz((int)(hi - lo)) : 0);
-    auto at_cut = [&](unsigned long long k) LC_INLINE { return shift == 64 ? true : ((k - base) >> shift) == 0ull; };
-    bool few = false;
-    while (!all && shift > 0 && !few) {
-        const int next = max(0, shift - LC_EV_DIGIT);
-        each([&](int, int n, unsigned long long k) LC_INLINE {
-            if (k != LC_EV_PINNED && at_cut(k)) atomicAdd(&tok_sh[(int)((k - base) >> next)], n);
+    if (!all)
+        lc_cut_search(sh, lc_cut_of(lo, hi, left), false, M, each, [&](int j, int* n) LC_INLINE {
+            const int begin = bnd[j], end = bnd[j + 1];
+            *n = end - begin;
+            return key_of(j, begin, end);
         });
-        __syncthreads();
-        // from the largest digit down: thread t has digits (BINS - 1 - 2 t) and the one below
-        const int d1 = LC_EV_BINS - 1 - 2 * tid, t1 = tok_sh[d1], t0 = tok_sh[d1 - 1];
-        int total;
-        const int before = lc_block_scan<NT>(t1 + t0, scan_sh, &total);
-        if (before <= left && before + t1 > left) { found_sh[0] = d1; found_sh[1] = before; }
-        else if (before + t1 <= left && before + t1 + t0 > left) { found_sh[0] = d1 - 1; found_sh[1] = before + t1; }
-        tok_sh[d1] = tok_sh[d1 - 1] = 0;
-        __syncthreads();
-        base += (unsigned long long)found_sh[0] << next;
-        left -= found_sh[1];
-        shift = next;
-        // the chunks at the cut, if they are few
-        each([&](int j, int n, unsigned long long k) LC_INLINE {
-            if (k != LC_EV_PINNED && at_cut(k)) {
-                const int i = atomicAdd(&few_sh, 1);
-                if (i < LC_EV_FEW) {
-                    key_sh[i] = k;
-                    id_sh[i] = j;
-                    len_sh[i] = n;
-                }
-            }
-        });
-        __syncthreads();
-        few = few_sh <= LC_EV_FEW;
-        if (!few) {
-            __syncthreads();
-            if (tid == 0) few_sh = 0;
-            __syncthreads();
-        }
-    }
-    // Every chunk up to (last_key, last_id) in the order is kept.
-    if (few) {
-        // a lane has a chunk at the cut, each wavefront some of those to compare it with
-        const int n = few_sh;
-        const unsigned long long k = lane < n ? key_sh[lane] : 0ull;
-        const int id = lane < n ? id_sh[lane] : 0x7fffffff;
-        int part = 0;
-        for (int i = wave; i < n; i += NW) {
-            const unsigned long long ki = key_sh[i];
-            if (ki > k || (ki == k && id_sh[i] <= id)) part += len_sh[i];
-        }
-        if (lane < n && part != 0) atomicAdd(&sum_sh[lane], part);
-        __syncthreads();
-        if (wave == 0) {
-            // (the sums of those that fit grow along the order: the last of them has the largest)
-            const int sum = sum_sh[lane];
-            const uint32_t mine = lane < n && sum <= left ? (uint32_t)sum + 1u : 0u;
-            const uint32_t most = (uint32_t)lc_readlane((int)lc_wave_extreme<true>(mine), 63);
-            if (most == 0u) {
-                if (lane == 0) last_key_sh = base + ((1ull << shift) - 1ull);    // none at the cut
-            } else if (mine == most) {
-                last_key_sh = k;
-                last_id_sh = id;
-            }
-        }
-    }
-    if (!all && !few) {
-        // equal keys at the cut: the first of them
-        int tied = 0;
-        for (int j0 = 0; j0 < M; j0 += NT) {
-            const int j = j0 + tid;
-            int n = 0;
-            if (j < M) {
-                const int begin = bnd[j], end = bnd[j + 1];
-                if (key_of(j, begin, end) == base) n = end - begin;
-            }
-            int total;
-            const int before = lc_block_scan<NT>(n, scan_sh, &total);
-            if (n > 0 && before <= left - tied - n) atomicMax(&last_id_sh, j);
-            tied = min(tied + total, 1 << 30);
-        }
-        if (tid == 0) last_key_sh = base;
-    }
-    __syncthreads();
-    const unsigned long long last_key = all ? 0ull : last_key_sh;
-    const int last_id = all ? 0x7fffffff : last_id_sh;
+    const unsigned long long last_key = all ? 0ull : sh.last_key;
+    const int last_id = all ? 0x7fffffff : sh.last_id;
     auto keeps = [&](unsigned long long k, int j) LC_INLINE { return k > last_key || (k == last_key && j <= last_id); };   // (pinned ones too)
 
     // ids, boundaries, the rest of both lists
@@ -500,15 +582,10 @@ lc_evict_select_kernel(const LcEvictArgs a) {
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int j = tid + c * NT;
-            int count = 0, tokens = 0;
-            if (c * NT < M) {
-                const bool k = j < M && keeps(key[c], j);
-                kept |= k ? 1u << c : 0u;
-                const int n = k ? len[c] : 0;
-                tokens = lc_wave_scan_incl(n);
-                len[c] = tokens - n;                         // (from here on: tokens kept before it, of the wavefront)
-                count = __popcll(__ballot(k));
-            }
+            const bool k = j < M && keeps(key[c], j);
+            kept |= k ? 1u << c : 0u;
+            const int n = k ? len[c] : 0, tokens = lc_wave_scan_incl(n), count = __popcll(__ballot(k));
+            len[c] = tokens - n;                             // (from here on: tokens kept before it, of the wavefront)
             if (lane == 63) { slab_cnt[c * NW + wave] = count; slab_tok[c * NW + wave] = tokens; }
         }
         __syncthreads();
@@ -523,52 +600,28 @@ lc_evict_select_kernel(const LcEvictArgs a) {
                 cc += lc_readlane(ci, 63);
                 tt += lc_readlane(ti, 63);
             }
-            if (lane == 0) { found_sh[0] = cc; found_sh[1] = tt; }
+            if (lane == 0) { sh.found[0] = cc; sh.found[1] = tt; }
         }
         __syncthreads();
 #pragma unroll
-        for (int c = 0; c < C; ++c)
-            if (c * NT < M) {
-                const bool k = (kept >> c) & 1u;
-                const int i = slab_cnt[c * NW + wave] + __popcll(__ballot(k) & ((1ull << lane) - 1ull));
-                if (k) {
-                    ids[i] = tid + c * NT;
-                    bounds[i] = slab_tok[c * NW + wave] + len[c];
-                }
+        for (int c = 0; c < C; ++c) {
+            const bool k = (kept >> c) & 1u;
+            const int i = slab_cnt[c * NW + wave] + __popcll(__ballot(k) & ((1ull << lane) - 1ull));
+            if (k) {
+                ids[i] = tid + c * NT;
+                bounds[i] = slab_tok[c * NW + wave] + len[c];
             }
-        n_keep = found_sh[0];
-        n_tok = found_sh[1];
+        }
+        n_keep = sh.found[0];
+        n_tok = sh.found[1];
     }
-    // (a thread has four chunks in a row: a scan for 4096)
-    for (int j0 = C * NT; j0 < M; j0 += 4 * NT) {
-        const int j = j0 + 4 * tid;
-        int edge[5];
-        unsigned long long k[4];
-#pragma unroll
-        for (int u = 0; u < 5; ++u) edge[u] = bnd[min(j + u, M)];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) k[u] = all ? 0ull : key_of(min(j + u, M - 1), edge[u], edge[u + 1]);
+    if (__builtin_expect(M > C * NT, 0)) lc_evict_place(C * NT, M, bnd, ids, bounds, sh.scan, n_keep, n_tok, [&](int j, const int* edge) LC_INLINE {
         uint32_t kept = 0u;
-        int n = 0;
 #pragma unroll
         for (int u = 0; u < 4; ++u)
-            if (j + u < M && keeps(k[u], j + u)) {
-                kept |= 1u << u;
-                n += edge[u + 1] - edge[u];
-            }
-        int at, to, count, tokens;
-        lc_block_scan2<NT>(__popc(kept), n, scan_sh, &at, &to, &count, &tokens);
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-            if ((kept >> u) & 1u) {
-                ids[n_keep + at] = j + u;
-                bounds[n_keep + at] = n_tok + to;
-                at += 1;
-                to += edge[u + 1] - edge[u];
-            }
-        n_keep += count;
-        n_tok += tokens;
-    }
+            kept |= j + u < M && (all || keeps(key_of(min(j + u, M - 1), edge[u], edge[u + 1]), j + u)) ? 1u << u : 0u;
+        return kept;
+    });
     for (int i = n_keep + tid; i < ix.cap[0]; i += NT) {
         ids[i] = -1;
         bounds[i] = n_tok;
@@ -577,6 +630,219 @@ lc_evict_select_kernel(const LcEvictArgs a) {
         bounds[ix.cap[0]] = n_tok;
         a.counts[b] = n_keep;
         if (a.lens) a.lens[b] = n_tok + max(0, T - last);
+    }
+}
+
+// ---- many chunks: several workgroups to a sequence, each with a range of its chunks
+// One alone reads the keys at what a compute unit gets from its L2, and several times.  Three launches behind the keys': the first digit's tokens, added up by all, and by
+// the last one to arrive the cut; the chunks above it, counted, those at it, listed, and by the last one the rest of the search among them; ids and boundaries.
+// Bound by the four launches, each a few trips to memory long: 26 K chunks 24 us (by one workgroup 43), 87 K 28 (142).
+struct LcSlab {
+    int lo, hi;           // chunks of this workgroup
+    int size;             // of each
+    __device__ __forceinline__ LcSlab(int M, int part, int parts) {
+        size = ((M + parts - 1) / parts + LC_EV_SLAB - 1) / LC_EV_SLAB * LC_EV_SLAB;
+        lo = min(M, (int)min((long long)part * size, (long long)M));
+        hi = min(M - lo, size) + lo;
+    }
+};
+// f(chunk, tokens, key, whether there is one) of a workgroup's chunks, in any order, by whole wavefronts
+template <typename F>
+__device__ __forceinline__ void lc_slab_each(const LcSlab& slab, const int* bnd, const unsigned long long* keys, F f) {
+    constexpr int U = LC_EV_SLAB / LC_EV_THREADS;
+    for (int j0 = slab.lo; j0 < slab.hi; j0 += LC_EV_SLAB) {
+        int n[U];
+        unsigned long long k[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int j = min(j0 + u * LC_EV_THREADS + (int)threadIdx.x, slab.hi - 1);
+            n[u] = bnd[j + 1] - bnd[j];
+            k[u] = keys[j];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int j = j0 + u * LC_EV_THREADS + (int)threadIdx.x;
+            f(j, n[u], k[u], j < slab.hi);
+        }
+    }
+}
+
+__global__ void __launch_bounds__(LC_EV_THREADS)
+lc_evict_cut_kernel(const LcEvictArgs a) {
+    lc_fetch_args<sizeof(LcEvictArgs)>();
+    __shared__ LcCutSh sh;
+    const LcDev& ix = a.ix;
+    const int b = blockIdx.y, tid = threadIdx.x, M = min(ix.state[b * ix.H * 4 + 1], ix.cap[0]);
+    const int* bnd = ix.bounds + (size_t)b * (ix.cap[0] + 1);
+    int32_t* spare = a.spare + (size_t)b * 2 * ix.cap[0];
+    const int last = bnd[M];
+    int tok = 0;
+    uint32_t lo = 0xffffffffu, hi = 0u;
+    lc_evict_range(a, b, lo, hi, tok);
+    lc_cut_prepare(sh);
+    lo = (uint32_t)lc_readlane((int)lc_wave_extreme<false>(lo), 63);
+    hi = (uint32_t)lc_readlane((int)lc_wave_extreme<true>(hi), 63);
+    const int others = lc_readlane(lc_wave_scan_incl(tok), 63), left = max(0, a.keep - (last - others));
+    if (others <= left) {                                    // (all stay)
+        if (blockIdx.x == 0 && tid == 0) spare[LC_EVS_CUT + 3] = -1;
+        return;
+    }
+    LcCut cut = lc_cut_of(lo, hi, left);
+    __syncthreads();
+    lc_slab_each(LcSlab(M, blockIdx.x, gridDim.x), bnd, a.keys + (size_t)b * ix.cap[0], [&](int, int n, unsigned long long k, bool real) LC_INLINE {
+        int d;
+        if (cut.digit(k, &d) && real) atomicAdd(&sh.tok[d], n);
+    });
+    __syncthreads();
+    for (int i = tid; i < LC_EV_BINS; i += LC_EV_THREADS)
+        if (sh.tok[i] != 0) __hip_atomic_fetch_add(spare + i, sh.tok[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (!lc_arrive_last(&ix.sync[b * ix.H * 4 + 2], gridDim.x, &sh.few)) return;
+    const uint32_t* digits = reinterpret_cast<const uint32_t*>(spare);
+    const int d1 = LC_EV_BINS - 1 - 2 * tid, t1 = (int)lc_load_agent(digits + d1), t0 = (int)lc_load_agent(digits + d1 - 1);
+    lc_cut_digit(sh, cut, t1, t0, false);
+    if (tid == 0) {
+        spare[LC_EVS_CUT] = (int32_t)(uint32_t)cut.base;
+        spare[LC_EVS_CUT + 1] = (int32_t)(uint32_t)(cut.base >> 32);
+        spare[LC_EVS_CUT + 2] = cut.shift;
+        spare[LC_EVS_CUT + 3] = cut.left;
+        ix.sync[b * ix.H * 4 + 2] = 0;                       // ready for the next launch
+    }
+}
+
+__global__ void __launch_bounds__(LC_EV_THREADS)
+lc_evict_sift_kernel(const LcEvictArgs a) {
+    lc_fetch_args<sizeof(LcEvictArgs)>();
+    constexpr int NW = LC_EV_THREADS / 64;
+    __shared__ LcCutSh sh;
+    __shared__ int red_sh[2 * NW];
+    const LcDev& ix = a.ix;
+    const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, M = min(ix.state[b * ix.H * 4 + 1], ix.cap[0]);
+    const int* bnd = ix.bounds + (size_t)b * (ix.cap[0] + 1);
+    const unsigned long long* keys = a.keys + (size_t)b * ix.cap[0];
+    int32_t* spare = a.spare + (size_t)b * 2 * ix.cap[0];
+    int32_t* const list = spare + LC_EVS_RANGE + 3 * a.sums;
+    const LcSlab slab(M, blockIdx.x, gridDim.x);
+    const LcCut cut = {(unsigned long long)(uint32_t)spare[LC_EVS_CUT] | (unsigned long long)(uint32_t)spare[LC_EVS_CUT + 1] << 32, spare[LC_EVS_CUT + 2], spare[LC_EVS_CUT + 3]};
+    lc_cut_prepare(sh);
+    uint32_t* const mine = reinterpret_cast<uint32_t*>(spare + LC_EVS_KEPT + 2 * blockIdx.x);
+    if (cut.left < 0) {                                      // (all stay)
+        if (tid == 0) {
+            mine[0] = (uint32_t)(slab.hi - slab.lo);
+            mine[1] = (uint32_t)(bnd[slab.hi] - bnd[slab.lo]);
+            if (blockIdx.x == 0) { spare[LC_EVS_LAST] = spare[LC_EVS_LAST + 1] = 0; spare[LC_EVS_LAST + 2] = 0x7fffffff; }
+        }
+        return;
+    }
+    int count = 0, tokens = 0;
+    lc_slab_each(slab, bnd, keys, [&](int j, int n, unsigned long long k, bool real) LC_INLINE {
+        const bool above = real && cut.above(k), at = real && cut.at(k);
+        count += above ? 1 : 0;
+        tokens += above ? n : 0;
+        const unsigned long long m = __ballot(at);
+        if (m != 0ull) {
+            int place = 0;
+            if (lane == 0) place = __hip_atomic_fetch_add(spare + LC_EVS_N, __popcll(m), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            place = lc_readlane(place, 0) + __popcll(m & ((1ull << lane) - 1ull));
+            if (at) lc_store_agent(reinterpret_cast<uint32_t*>(list + place), (uint32_t)j);
+        }
+    });
+    count = lc_wave_scan_incl(count);
+    tokens = lc_wave_scan_incl(tokens);
+    if (lane == 63) { red_sh[wave] = count; red_sh[NW + wave] = tokens; }
+    __syncthreads();
+    if (tid == 0) {
+        count = tokens = 0;
+        for (int w = 0; w < NW; ++w) { count += red_sh[w]; tokens += red_sh[NW + w]; }
+        lc_store_agent(mine, (uint32_t)count);
+        lc_store_agent(mine + 1, (uint32_t)tokens);
+    }
+    if (!lc_arrive_last(&ix.sync[b * ix.H * 4 + 2], gridDim.x, red_sh)) return;
+    // the chunks at the cut: one in a thread's registers, the others, if there are so many, where they are
+    const int listed = min((int)lc_load_agent(reinterpret_cast<const uint32_t*>(spare + LC_EVS_N)), M);
+    auto entry = [&](int i, int* n, unsigned long long* k) LC_INLINE -> int {
+        const int j = min((int)lc_load_agent(reinterpret_cast<const uint32_t*>(list + i)), M - 1);
+        *n = bnd[j + 1] - bnd[j];
+        *k = keys[j];
+        return j;
+    };
+    int j1 = 0, n1 = 0;
+    unsigned long long k1 = LC_EV_PINNED;
+    if (tid < listed) j1 = entry(tid, &n1, &k1);
+    auto each = [&](auto f) LC_INLINE {
+        f(j1, n1, k1);
+        for (int i = tid + LC_EV_THREADS; i < listed; i += LC_EV_THREADS) {
+            int n;
+            unsigned long long k;
+            const int j = entry(i, &n, &k);
+            f(j, n, k);
+        }
+    };
+    lc_cut_search(sh, cut, true, M, each, [&](int j, int* n) LC_INLINE {
+        *n = bnd[j + 1] - bnd[j];
+        return keys[j];
+    });
+    const unsigned long long last_key = sh.last_key;
+    const int last_id = sh.last_id;
+    each([&](int j, int n, unsigned long long k) LC_INLINE {
+        if (k != LC_EV_PINNED && (k > last_key || (k == last_key && j <= last_id))) {
+            int32_t* const whose = spare + LC_EVS_KEPT + 2 * (j / slab.size);
+            __hip_atomic_fetch_add(whose, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __hip_atomic_fetch_add(whose + 1, n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+    });
+    if (tid == 0) {
+        spare[LC_EVS_LAST] = (int32_t)(uint32_t)last_key;
+        spare[LC_EVS_LAST + 1] = (int32_t)(uint32_t)(last_key >> 32);
+        spare[LC_EVS_LAST + 2] = last_id;
+        ix.sync[b * ix.H * 4 + 2] = 0;                       // ready for the next launch
+    }
+}
+
+__global__ void __launch_bounds__(LC_EV_THREADS)
+lc_evict_place_kernel(const LcEvictArgs a) {
+    lc_fetch_args<sizeof(LcEvictArgs)>();
+    __shared__ int scan_sh[2 * (LC_EV_THREADS / 64)];
+    const LcDev& ix = a.ix;
+    const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, T = ix.state[b * ix.H * 4 + 0], M = min(ix.state[b * ix.H * 4 + 1], ix.cap[0]);
+    const int* bnd = ix.bounds + (size_t)b * (ix.cap[0] + 1);
+    const unsigned long long* keys = a.keys + (size_t)b * ix.cap[0];
+    const int32_t* spare = a.spare + (size_t)b * 2 * ix.cap[0];
+    const LcSlab slab(M, blockIdx.x, gridDim.x);
+    const unsigned long long last_key = (unsigned long long)(uint32_t)spare[LC_EVS_LAST] | (unsigned long long)(uint32_t)spare[LC_EVS_LAST + 1] << 32;
+    const int last_id = spare[LC_EVS_LAST + 2], last = bnd[M];
+    // what the workgroups before this one keep, and all
+    int n_keep = 0, n_tok = 0, all_keep = 0, all_tok = 0;
+    for (int i = lane; i < (int)gridDim.x; i += 64) {
+        const int c = spare[LC_EVS_KEPT + 2 * i], t = spare[LC_EVS_KEPT + 2 * i + 1];
+        all_keep += c;
+        all_tok += t;
+        n_keep += i < (int)blockIdx.x ? c : 0;
+        n_tok += i < (int)blockIdx.x ? t : 0;
+    }
+    auto sum = [&](int v) LC_INLINE { return lc_readlane(lc_wave_scan_incl(v), 63); };
+    n_keep = sum(n_keep);
+    n_tok = sum(n_tok);
+    all_keep = sum(all_keep);
+    all_tok = sum(all_tok);
+    int32_t* ids = a.ids + (size_t)b * ix.cap[0];
+    int32_t* bounds = a.bounds + (size_t)b * (ix.cap[0] + 1);
+    lc_evict_place(slab.lo, slab.hi, bnd, ids, bounds, scan_sh, n_keep, n_tok, [&](int j, const int*) LC_INLINE {
+        uint32_t kept = 0u;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const unsigned long long k = keys[min(j + u, slab.hi - 1)];
+            kept |= j + u < slab.hi && (k > last_key || (k == last_key && j + u <= last_id)) ? 1u << u : 0u;
+        }
+        return kept;
+    });
+    for (int i = all_keep + (int)blockIdx.x * LC_EV_THREADS + tid; i < ix.cap[0]; i += (int)gridDim.x * LC_EV_THREADS) {
+        ids[i] = -1;
+        bounds[i] = all_tok;
+    }
+    if (blockIdx.x == 0 && tid == 0) {
+        bounds[ix.cap[0]] = all_tok;
+        a.counts[b] = all_keep;
+        if (a.lens) a.lens[b] = all_tok + max(0, T - last);
     }
 }
 
@@ -805,8 +1071,8 @@ int lc_evict_select(const lc_index* idx, const float* weights, int keep_tokens, 
                     int32_t* keep_counts, int32_t* keep_lens, void* ws, size_t ws_bytes, void* stream) {
     if (!idx || !weights || !keep_ids || !keep_bounds || !keep_counts || !ws || !aligned(ws, 256)) return LC_ERR_INVALID_ARG;
     if (keep_tokens < 0 || recent_tokens < 0) return LC_ERR_INVALID_ARG;
-    const size_t need = (size_t)idx->B * idx->cfg.max_chunks * sizeof(unsigned long long);
-    if (ws_bytes < need) return LC_ERR_WORKSPACE_TOO_SMALL;
+    const size_t keys_bytes = (size_t)idx->B * idx->cfg.max_chunks * sizeof(unsigned long long);
+    if (ws_bytes < (idx->cfg.max_chunks > LC_EV_SINGLE_MAX ? 2 * keys_bytes : keys_bytes)) return LC_ERR_WORKSPACE_TOO_SMALL;
     unsigned long long* keys = static_cast<unsigned long long*>(ws);
     hipStream_t st = static_cast<hipStream_t>(stream);
     int most = 0;
@@ -819,14 +1085,30 @@ int lc_evict_select(const lc_index* idx, const float* weights, int keep_tokens, 
     a.ids = keep_ids; a.bounds = keep_bounds; a.counts = keep_counts; a.lens = keep_lens;
     a.keep = keep_tokens; a.recent = recent_tokens; a.sink = idx->cfg.sink_tokens;
     a.sums = (most + LC_EV_SUM - 1) / LC_EV_SUM;
+    a.range = keep_ids;                                      // (room for more than that, and written behind all else)
+    a.range_seq = idx->cfg.max_chunks;
+    a.spare = nullptr;
     const dim3 grid(idx->B), block(LC_EV_THREADS);
     if (most <= LC_EV_FUSED_MAX) {
         if (most <= LC_EV_THREADS) hipLaunchKernelGGL((lc_evict_select_kernel<1, true>), grid, block, 0, st, a);
         else hipLaunchKernelGGL((lc_evict_select_kernel<4, true>), grid, block, 0, st, a);
-    } else {
+    } else if (most <= LC_EV_SINGLE_MAX) {
         hipLaunchKernelGGL(lc_evict_keys_kernel, dim3(a.sums, idx->B), dim3(LC_EV_SUM), 0, st, a);
         LC_HIP_CHECK(hipGetLastError());
         hipLaunchKernelGGL((lc_evict_select_kernel<12, false>), grid, block, 0, st, a);
+    } else {
+        a.spare = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + keys_bytes);
+        a.range = a.spare + LC_EVS_RANGE;
+        a.range_seq = 2 * (long long)idx->cfg.max_chunks;
+        const int slabs = (most + LC_EV_SLAB - 1) / LC_EV_SLAB;
+        const dim3 shared(slabs < LC_EV_GROUPS ? slabs : LC_EV_GROUPS, idx->B);
+        hipLaunchKernelGGL(lc_evict_keys_kernel, dim3(a.sums, idx->B), dim3(LC_EV_SUM), 0, st, a);
+        LC_HIP_CHECK(hipGetLastError());
+        hipLaunchKernelGGL(lc_evict_cut_kernel, shared, block, 0, st, a);
+        LC_HIP_CHECK(hipGetLastError());
+        hipLaunchKernelGGL(lc_evict_sift_kernel, shared, block, 0, st, a);
+        LC_HIP_CHECK(hipGetLastError());
+        hipLaunchKernelGGL(lc_evict_place_kernel, shared, block, 0, st, a);
     }
     LC_HIP_CHECK(hipGetLastError());
     return LC_OK;

@@ -224,6 +224,51 @@ def test_selection_among_many(C):
             _check_select(C, c, w.astype(np.float32), keep, recent, 0)
 
 
+@pytest.mark.parametrize("H,chunks", [(2, (30000, 5, 14000)), (1, (14337, 13000, 0))])
+def test_selection_by_several_workgroups(C, H, chunks):
+    """A sequence with more chunks than one workgroup takes, others of the batch with fewer or none."""
+    r = np.random.default_rng(H)
+    bounds = [np.concatenate([[0], np.cumsum(r.integers(1, 3, size=n))]) for n in chunks]
+    c = C.Cache(66, H, 1, [int(x[-1]) + 3 for x in bounds], bounds, sink=21)
+    shape, n = (3, H, c.cfg.max_chunks), int(bounds[0][-1])
+    spread = np.exp(3 * r.standard_normal(shape))
+    for w in (spread, np.where(r.random(shape) < 0.2, spread, 0), np.zeros(shape), np.where(r.random(shape) < 0.1, np.nan, spread),
+              1 + r.integers(0, 3, size=shape) * 2.0 ** -23, np.where(r.random(shape) < 0.5, np.inf, -spread)):
+        for keep, recent in ((0, 0), (1, 300), (n // 3, 64), (n - 1, 0), (n, 0)):
+            _check_select(C, c, w.astype(np.float32), keep, recent, 21)
+
+
+@pytest.mark.parametrize("chunks", [4096, 12288, 14336, 14337])
+def test_captured_selection_of_a_growing_index(C, chunks):
+    """The launches are chosen when they are captured; later calls have other weights and more chunks."""
+    import torch
+    lc = C.lc
+    c = C.Cache(67, 1, 1, [chunks], [np.arange(chunks + 1)], extra=6, extra_chunks=6)
+    M = c.cfg.max_chunks
+    w = torch.zeros(1, 1, M, device="cuda")
+    got = [torch.zeros(1, n, dtype=torch.int32, device="cuda") for n in (M, M + 1)] + [torch.zeros(1, dtype=torch.int32, device="cuda") for _ in range(2)]
+    call = lambda: lc.lc_evict_select(c.idx, w, 3000, 9, got[0], got[1], got[2], c.ws, keep_lens=got[3])
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    row = torch.zeros(1, 1, 128, dtype=torch.bfloat16, device="cuda")
+    for step in range(4):
+        now = np.exp(c.r.standard_normal((1, 1, M))).astype(np.float32)
+        w.copy_(torch.from_numpy(now))
+        graph.replay()
+        torch.cuda.synchronize()
+        bounds = np.arange(chunks + step + 1)
+        want = c4.keep(now[0, :, :chunks + step], bounds, 3000, 9, 0)
+        assert int(got[2]) == len(want) == int(got[3]) and got[0][0, :len(want)].tolist() == want and (got[0][0, len(want):] == -1).all()
+        eager = _select(C, c, now, 3000, 9)
+        assert all(torch.equal(x, y) for x, y in zip(got, eager))
+        lc.lc_append(c.idx, c.K, c.V, row, row, [1], c.ws)
+
+
 # ------------------------------------------------------------------ rows
 
 @pytest.mark.parametrize("bits", [16, 4])
