@@ -16,7 +16,7 @@
 // per 32 would take the rows as they are, with the query in two e4m3 terms that hold it exactly: it adds up its products aligned to the largest of them,
 // 4.5e-5 of the result's size off on random operands of that kind.)
 //
-// Measured (kernel alone, replayed from a graph, cold rows): 1024 of 4K tokens, 8 heads of group size 4, 8.8 us; 4096 of 128K tokens 10.0; 16 ragged sequences, 4
+// Measured (kernel alone, replayed from a graph, cold rows): 1024 of 4K tokens, 8 heads of group size 4, 8.6 us; 4096 of 128K tokens 9.8 (8.75 and 9.95 with the long lists' code between the other in the kernel); 16 ragged sequences, 4
 // heads of group size 7, 2048 tokens each 14.3; all of 4 x 128K tokens 119 (570 MB: 4.8 TB/s, one behind the other 5.2).  lc_sparse_decode over bfloat16 rows: 8.2, 10.9, 19.1 and 390.
 // Long lists are bound by the bytes: without arithmetic the last one takes 4 us less, with all rows from the caches 96.  Short ones are a chain: launch 2.6, ids and
 // boundaries 0.4, rows' places 1.4, a step 1.5, sums through LDS 0.9, arrival 1.2, merge 1.9.
@@ -212,7 +212,7 @@ lc_decode4_kernel(const LcDecode4Args a) {
     const bool long_list = n_ids > PASS;
     const int passes = (n_ids + PASS - 1) / PASS, per_slot = (passes + 63) / 64;
     int n_sel = tot0, slot_end = 0;                          // (lane l: tokens up to the end of slot l)
-    if (long_list) {
+    if (__builtin_expect(long_list, 0)) {
         Ids next = load_ids(PASS);
         for (int p = 1; p < passes; ++p) {
             const Ids now = next;
@@ -386,7 +386,7 @@ lc_decode4_kernel(const LcDecode4Args a) {
             }
         };
         if (tile0 != lo) __syncthreads();                           // the previous tile's rows have been used
-        if (!long_list) {
+        if (__builtin_expect(!long_list, 1)) {
             place(0, ex0, tot0, n_ids, st0, ln0);
         } else {
             const unsigned long long behind = __ballot(slot_end > tile0);
