@@ -487,15 +487,25 @@ lc_decode4_kernel(const LcDecode4Args a) {
     const int v = tid % NV, wy = tid / NV;
     const int g = v / (LC_D / 4), c4 = v % (LC_D / 4);
     float4 x[MR];
-    auto load_round = [&](int sp0) LC_INLINE {               // (past the last split: zeros)
+    auto load_round = [&](int sp0) LC_INLINE {               // (by eights, as many as there are; past the last split: zeros)
 #pragma unroll
-        for (int k = 0; k < MR; ++k) x[k] = lc_load_agent4(pacc_r, (((sp0 + k * WAYS) * G + g) * LC_D + 4 * c4) * 4);
+        for (int k0 = 0; k0 < MR; k0 += 8)
+            if (sp0 + k0 * WAYS < S_eff) {
+#pragma unroll
+                for (int k = k0; k < k0 + 8; ++k) x[k] = lc_load_agent4(pacc_r, (((sp0 + wy + k * WAYS) * G + g) * LC_D + 4 * c4) * 4);
+            }
     };
-    load_round(wy);
+    load_round(0);
     // Every 32 lanes have one head (slot v of the output) and turn its splits' references and sums into scales by themselves.
     const int half = tid >> 5, hl = tid & 31;
-    float m_all = LC_NEG_INF, den = 0.f;
-    for (int sp = hl; sp < S_eff; sp += 32) {
+    float den = 0.f;
+    float m0 = LC_NEG_INF, l0 = 0.f;                         // (the first 32 stay in registers)
+    if (hl < S_eff) {
+        m0 = lc_load_agent(pml + 2 * (hl * G + g));
+        l0 = lc_load_agent(pml + 2 * (hl * G + g) + 1);
+    }
+    float m_all = m0;
+    for (int sp = hl + 32; sp < S_eff; sp += 32) {
         const float m = lc_load_agent(pml + 2 * (sp * G + g)), l = lc_load_agent(pml + 2 * (sp * G + g) + 1);
         ph.merge.scale[half][sp] = m;
         ph.merge.sum[half][sp] = l;
@@ -510,10 +520,10 @@ lc_decode4_kernel(const LcDecode4Args a) {
         m_all = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
     }
     const float ref = m_all == LC_NEG_INF ? 0.f : m_all;
-    const int n_slots = (S_eff + MR * WAYS - 1) / (MR * WAYS) * (MR * WAYS);
+    const int n_slots = (S_eff + 8 * WAYS - 1) / (8 * WAYS) * (8 * WAYS);
     for (int sp = hl; sp < n_slots; sp += 32) {              // (this lane's own entries; up to the end of the last round, where sums are zero)
-        const float f = sp < S_eff ? __builtin_amdgcn_exp2f(ph.merge.scale[half][sp] - ref) : 0.f;
-        if (sp < S_eff) den = fmaf(ph.merge.sum[half][sp], f, den);
+        const float f = sp >= S_eff ? 0.f : __builtin_amdgcn_exp2f((sp < 32 ? m0 : ph.merge.scale[half][sp]) - ref);
+        if (sp < S_eff) den = fmaf(sp < 32 ? l0 : ph.merge.sum[half][sp], f, den);
         ph.merge.scale[half][sp] = f;
     }
     den = lc_sum16(den);
@@ -522,14 +532,18 @@ lc_decode4_kernel(const LcDecode4Args a) {
     __builtin_amdgcn_wave_barrier();
     float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
     if (wy < WAYS) {
-        for (int sp0 = wy; sp0 < S_eff; sp0 += MR * WAYS) {
-            if (sp0 != wy) load_round(sp0);
+        for (int sp0 = 0; sp0 < S_eff; sp0 += MR * WAYS) {
+            if (sp0 != 0) load_round(sp0);
 #pragma unroll
-            for (int k = 0; k < MR; ++k) {
-                const float f = ph.merge.scale[half][sp0 + k * WAYS];
-                num.x = fmaf(x[k].x, f, num.x); num.y = fmaf(x[k].y, f, num.y);
-                num.z = fmaf(x[k].z, f, num.z); num.w = fmaf(x[k].w, f, num.w);
-            }
+            for (int k0 = 0; k0 < MR; k0 += 8)
+                if (sp0 + k0 * WAYS < S_eff) {
+#pragma unroll
+                    for (int k = k0; k < k0 + 8; ++k) {
+                        const float f = ph.merge.scale[half][sp0 + wy + k * WAYS];
+                        num.x = fmaf(x[k].x, f, num.x); num.y = fmaf(x[k].y, f, num.y);
+                        num.z = fmaf(x[k].z, f, num.z); num.w = fmaf(x[k].w, f, num.w);
+                    }
+                }
         }
     }
     if (WAYS > 1) {
