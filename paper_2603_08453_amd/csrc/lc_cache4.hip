@@ -16,12 +16,14 @@
 // per 32 would take the rows as they are, with the query in two e4m3 terms that hold it exactly: it adds up its products aligned to the largest of them,
 // 4.5e-5 of the result's size off on random operands of that kind.)
 //
-// Measured (kernel alone, replayed from a graph, cold rows): 1024 of 4K tokens, 8 heads of group size 4, 8.6 us; 4096 of 128K tokens 9.8 (8.75 and 9.95 with the long lists' code between the other in the kernel); 16 ragged sequences, 4
-// heads of group size 7, 2048 tokens each 14.3; all of 4 x 128K tokens 119 (570 MB: 4.8 TB/s, one behind the other 5.2).  lc_sparse_decode over bfloat16 rows: 8.2, 10.9, 19.1 and 390.
-// Long lists are bound by the bytes: without arithmetic the last one takes 4 us less, with all rows from the caches 96.  Short ones are a chain: launch 2.6, ids and
-// boundaries 0.4, rows' places 1.4, a step 1.5, sums through LDS 0.9, arrival 1.2, merge 1.9.
+// Measured (kernel alone, replayed from a graph, cold rows): 1024 of 4K tokens, 8 heads of group size 4, 8.2 us; 4096 of 128K tokens 9.7
+// (with the long lists' code between the other in the kernel 0.1 more, with all 16 reads of a merging thread however few splits there are another 0.3); 16 ragged sequences, 4
+// heads of group size 7, 2048 tokens each 13.9; all of 4 x 128K tokens 119 (570 MB: 4.8 TB/s, one behind the other 5.2).  lc_sparse_decode over bfloat16 rows: 8.2, 10.9, 19.1 and 390.
+// Long lists are bound by the bytes: without arithmetic the last one takes 4 us less, with all rows from the caches 96.  Short ones are a chain: launch 1.4, the list 0.7,
+// boundaries and their sums 0.6, rows' places 1.4, rows 0.5, a step 0.9, sums through LDS and out 1.1, arrival 0.5, merge 1.2.
 // Other ways: three steps on their way instead of two 130.7 us (129 with two at that stage); three or four workgroups per compute unit spill registers; rows past
-// the caches 154 (lines that several loads share come twice); the list held by every wavefront, without barriers, 10.0 and 121.
+// the caches 154 (lines that several loads share come twice); the list held by every wavefront, without barriers, 10.0 and 121; rows found by each wavefront
+// for its own steps from marks that the entries leave at their first tokens, one barrier instead of three, 8.5 and 122.
 #include "lc_cache4.h"
 #include "lc_internal.h"
 #include "lc_select.h"
@@ -349,10 +351,8 @@ lc_decode4_kernel(const LcDecode4Args a) {
     };
 
     // ---- the split's tokens, in tiles whose rows the workgroup first writes into LDS
-    // tokens [n_tok s / S_eff, n_tok (s + 1) / S_eff), in 32 bits: with n_tok = each S_eff + more, more < S_eff <= 256
-    const uint32_t each = (uint32_t)n_tok / (uint32_t)S_eff, more = (uint32_t)n_tok % (uint32_t)S_eff;
-    const int lo = (int)(each * (uint32_t)s + more * (uint32_t)s / (uint32_t)S_eff);
-    const int hi = (int)(each * (uint32_t)(s + 1) + more * (uint32_t)(s + 1) / (uint32_t)S_eff);
+    const int each = (int)((uint32_t)n_tok / (uint32_t)S_eff), more = n_tok - each * S_eff;      // (the first `more` splits: one more)
+    const int lo = each * s + min(s, more), hi = lo + each + (s < more ? 1 : 0);
     const int row_max = max(T - 1, 0);
     for (int tile0 = lo; tile0 < hi; tile0 += LC_D4_TILE) {
         const int tl = min(LC_D4_TILE, hi - tile0);
