@@ -238,6 +238,24 @@ def test_selection_by_several_workgroups(C, H, chunks):
             _check_select(C, c, w.astype(np.float32), keep, recent, 21)
 
 
+@pytest.mark.parametrize("room,per", [(14336, 8), (14337, 16)])
+def test_workspace_of_the_selection(C, room, per):
+    """Its size goes by the room for chunks; a larger one is used no further."""
+    import torch
+    lc = C.lc
+    c = C.Cache(68, 1, 1, [300], [np.arange(301)], extra=room, extra_chunks=room - 300, sink=5)
+    w = np.exp(c.r.standard_normal((1, 1, room))).astype(np.float32)
+    ws = torch.full((per * room + 256,), 7, dtype=torch.uint8, device="cuda")
+    out = [torch.zeros(1, n, dtype=torch.int32, device="cuda") for n in (room, room + 1, 1)]
+    with pytest.raises(lc.LycheeError) as e:
+        lc.lc_evict_select(c.idx, torch.from_numpy(w).cuda(), 100, 0, *out, ws[:per * room - 1])
+    assert e.value.code == lc.LC_ERR_WORKSPACE_TOO_SMALL
+    lc.lc_evict_select(c.idx, torch.from_numpy(w).cuda(), 100, 0, *out, ws[:per * room])
+    torch.cuda.synchronize()
+    want = c4.keep(w[0, :, :300], np.arange(301), 100, 0, 5)
+    assert out[0][0, :int(out[2])].tolist() == want and (ws[per * room:] == 7).all()
+
+
 @pytest.mark.parametrize("chunks", [4096, 12288, 14336, 14337])
 def test_captured_selection_of_a_growing_index(C, chunks):
     """The launches are chosen when they are captured; later calls have other weights and more chunks."""
