@@ -283,6 +283,7 @@ class Index:
         self.index_buf = index_buf
         self.B = B
         self.H_kv = H_kv
+        self.sizes = (B, H_kv, int(cfg.max_chunks), int(cfg.max_tokens))      # what it has room for
 
     def info(self, b: int):
         T, M = ctypes.c_int32(), ctypes.c_int32()
@@ -468,6 +469,15 @@ def _strides4(t) -> "ctypes.Array":
     return (ctypes.c_int64 * 3)(t.stride(0), t.stride(1), t.stride(2))
 
 
+def _cache4(K4, V4) -> None:
+    assert K4.shape == V4.shape and K4.stride() == V4.stride() and V4.element_size() == 1, "K4 and V4 must be of the same type, shape and strides"
+
+
+def _room(idx):
+    """(sequences, KV heads, max_chunks, max_tokens) of the index; None of an object that carries a handle alone."""
+    return getattr(idx, "sizes", None)
+
+
 def _done(rc, where: str) -> bool:
     """Whether the native module made the call; raises if the library refused it."""
     if rc is NotImplemented:
@@ -506,7 +516,7 @@ def lc_sparse_decode4(idx: Index, q, K4, V4, chunk_ids, counts, out, ws, lse=Non
     """lc_sparse_decode over a 4-bit cache (uint8 [B][H_kv][tokens][68])."""
     if _done((_fast_mod or _fast()).sparse_decode4(idx.address, q, K4, V4, chunk_ids, counts, out, ws, lse, stream), "lc_sparse_decode4"):
         return
-    assert K4.stride() == V4.stride() and V4.element_size() == 1
+    _cache4(K4, V4)
     _check(lib().lc_sparse_decode4(idx.handle, _ptr(q), _ptr(K4), _ptr(V4), _strides4(K4), _ptr(chunk_ids), _ptr(counts),
                                    chunk_ids.shape[2], q.shape[1], _ptr(out), _ptr(lse), _ptr(ws), ws.numel() * ws.element_size(),
                                    _stream(stream)), "lc_sparse_decode4")
@@ -519,7 +529,7 @@ def lc_append4(idx: Index, K4, V4, k_new, v_new, close_chunk: Optional[Sequence[
     cc = None
     if close_chunk is not None:
         cc = (ctypes.c_uint8 * len(close_chunk))(*[1 if c else 0 for c in close_chunk])
-    assert K4.stride() == V4.stride() and V4.element_size() == 1
+    _cache4(K4, V4)
     _check(lib().lc_append4(idx.handle, _ptr(K4), _ptr(V4), _strides4(K4), _ptr(k_new), _ptr(v_new), cc, _stream(stream)), "lc_append4")
 
 
@@ -552,10 +562,15 @@ def lc_evict_select(idx: Index, weights, keep_tokens: int, recent_tokens: int, k
 
 
 def lc_evict_rows(idx: Index, keep_ids, keep_bounds, keep_counts, K, V, K_to, V_to, weights=None, weights_to=None, stream=None) -> None:
-    """The kept chunks' rows and the open tail's from K and V to the front of K_to and V_to; bf16 caches, or 4-bit ones (uint8)."""
-    if _done((_fast_mod or _fast()).evict_rows(idx.address, keep_ids, keep_bounds, keep_counts, K, V, K_to, V_to, weights, weights_to, stream), "lc_evict_rows"):
+    """The kept chunks' rows and the open tail's from K and V to the front of K_to and V_to; bf16 caches, or 4-bit ones (uint8).
+    K_to and V_to: K's shape, with at least max_tokens rows."""
+    room = _room(idx)
+    if _done((_fast_mod or _fast()).evict_rows(idx.address, keep_ids, keep_bounds, keep_counts, K, V, K_to, V_to, weights, weights_to, stream, room), "lc_evict_rows"):
         return
-    assert K.stride() == V.stride() and K_to.stride() == V_to.stride()
+    assert K.shape == V.shape and K.stride() == V.stride() and K_to.shape == V_to.shape and K_to.stride() == V_to.stride()
+    assert K.shape[:2] == K_to.shape[:2] and K.shape[3] == K_to.shape[3] and (K.element_size() == 1 or K.shape[3] == LC_HEAD_DIM), "K_to must have K's sequences, heads and row"
+    assert K_to.shape[2] >= (room[3] if room else K.shape[2]) and (room is None or (K.shape[0] >= room[0] and K.shape[1] >= room[1])), \
+        "K_to and V_to must have room for the index's max_tokens rows"
     assert K.element_size() in (1, 2) and all(t.element_size() == K.element_size() for t in (V, K_to, V_to)), "caches must be all bfloat16 or all of 4 bits"
     call, strides = (lib().lc_evict_rows4, _strides4) if K.element_size() == 1 else (lib().lc_evict_rows, _strides3)
     _check(call(idx.handle, _ptr(keep_ids), _ptr(keep_bounds), _ptr(keep_counts), _ptr(K), _ptr(V), strides(K), _ptr(K_to), _ptr(V_to),

@@ -64,6 +64,16 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Py_RETURN_NONE;
 }
 
+// What the index has room for: {sequences, KV heads, chunks, tokens}; not known of an object that carries a handle alone.
+struct Room {
+    bool known = false;
+    int64_t n[4] = {0, 0, 0, 0};
+    int64_t B() const { return n[0]; }
+    int64_t H() const { return n[1]; }
+    int64_t chunks() const { return n[2]; }
+    int64_t tokens() const { return n[3]; }
+};
+
 // Positional arguments of one call.
 class Args {
   public:
@@ -96,6 +106,13 @@ class Args {
         PyObject* const v = PyNumber_Index(a_[i]);
         const int r = v ? (int)PyLong_AsUnsignedLongMask(v) : -1;
         Py_XDECREF(v);
+        return r;
+    }
+    Room room(int i) {
+        Room r;
+        if (!PyTuple_Check(a_[i]) || PyTuple_GET_SIZE(a_[i]) != 4) return r;
+        for (int k = 0; k < 4; ++k) r.n[k] = PyLong_AsLong(PyTuple_GET_ITEM(a_[i], k));
+        r.known = !PyErr_Occurred();
         return r;
     }
     lc_index* handle(int i) { return static_cast<lc_index*>(PyLong_AsVoidPtr(a_[i])); }
@@ -285,8 +302,8 @@ PyObject* append(PyObject*, PyObject* const* args, Py_ssize_t n) {
 
 // Strides of a 4-bit cache, in bytes.
 bool cache4_strides(const at::Tensor& K4, const at::Tensor& V4, int64_t (&s)[3]) {
-    if (!K4.strides().equals(V4.strides())) {
-        PyErr_SetString(PyExc_AssertionError, "K4 and V4 must have the same strides");
+    if (!K4.sizes().equals(V4.sizes()) || !K4.strides().equals(V4.strides())) {
+        PyErr_SetString(PyExc_AssertionError, "K4 and V4 must have the same shape and strides");
         return false;
     }
     if (K4.dim() != 4 || K4.size(3) != LC_CACHE4_ROW || K4.stride(3) != 1 || K4.element_size() != 1 || V4.element_size() != 1) {
@@ -454,10 +471,20 @@ PyObject* evict_select(PyObject*, PyObject* const* args, Py_ssize_t n) {
     });
 }
 
-// evict_rows(handle, keep_ids, keep_bounds, keep_counts, K, V, K_to, V_to, weights, weights_to, stream)
+// Whether every row that an eviction may write lies in the destination (both are caches of four dimensions).
+bool holds_rows(const at::Tensor& K, const at::Tensor& K_to, const Room& room, bool in4) {
+    const bool alike = K.size(0) == K_to.size(0) && K.size(1) == K_to.size(1) && K.size(3) == K_to.size(3) && (in4 || K.size(3) == LC_HEAD_DIM);
+    if (!alike || K_to.size(2) < (room.known ? room.tokens() : K.size(2)) || (room.known && (K.size(0) < room.B() || K.size(1) < room.H()))) {
+        PyErr_SetString(PyExc_AssertionError, "K_to and V_to must have K's sequences, heads and row, and room for the index's max_tokens rows");
+        return false;
+    }
+    return true;
+}
+
+// evict_rows(handle, keep_ids, keep_bounds, keep_counts, K, V, K_to, V_to, weights, weights_to, stream, room)
 PyObject* evict_rows(PyObject*, PyObject* const* args, Py_ssize_t n) {
     Args a(args, n);
-    if (!a.count(11)) return nullptr;
+    if (!a.count(12)) return nullptr;
     return guarded(a, [&](int* rc) {
         const at::Tensor *K = a.tensor(4), *V = a.tensor(5), *K_to = a.tensor(6), *V_to = a.tensor(7);
         if (!K || !V || !K_to || !V_to || a.foreign()) return false;
@@ -465,8 +492,9 @@ PyObject* evict_rows(PyObject*, PyObject* const* args, Py_ssize_t n) {
         int64_t s[3], st_to[3];
         for (const at::Tensor* t : {K, V, K_to, V_to})
             if (t->element_size() != (in4 ? 1 : 2)) return false;
-        if (in4 ? !cache4_strides(*K, *V, s) || !cache4_strides(*K_to, *V_to, st_to) : !cache_strides(*K, *V, false, s) || !cache_strides(*K_to, *V_to, false, st_to))
+        if (in4 ? !cache4_strides(*K, *V, s) || !cache4_strides(*K_to, *V_to, st_to) : !cache_strides(*K, *V, true, s) || !cache_strides(*K_to, *V_to, true, st_to))
             return true;
+        if (!holds_rows(*K, *K_to, a.room(11), in4)) return true;
         const int32_t* const ids = static_cast<const int32_t*>(a.ptr(1));
         const int32_t* const bounds = static_cast<const int32_t*>(a.ptr(2));
         const int32_t* const counts = static_cast<const int32_t*>(a.ptr(3));
