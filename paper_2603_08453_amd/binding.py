@@ -478,6 +478,28 @@ def _room(idx):
     return getattr(idx, "sizes", None)
 
 
+def _table(t, floats: bool, rows: int, row: int, name: str) -> None:
+    """t, if there is one, holds `rows` rows of `row` 32-bit numbers one behind the other (row 0: that many numbers, whatever its shape)."""
+    assert t is None or (t.is_contiguous() and t.element_size() == 4 and t.is_floating_point() == floats and t.numel() >= rows * (row or 1)
+                         and (row == 0 or t.dim() < 2 or t.shape[-1] == row)), \
+        f"{name} must be a contiguous {'float32' if floats else 'int32'} table with the index's room"
+
+
+def _keep_tables(room, keep_ids, keep_bounds, keep_counts) -> None:
+    if room:
+        _table(keep_ids, False, room[0], room[2], "keep_ids")
+        _table(keep_bounds, False, room[0], room[2] + 1, "keep_bounds")
+        _table(keep_counts, False, room[0], 0, "keep_counts")
+
+
+def _weigh_tables(room, q, chunk_ids, counts, lse, weights) -> None:
+    if room:
+        _table(chunk_ids, False, room[0] * room[1], chunk_ids.shape[-1], "chunk_ids")
+        _table(counts, False, room[0] * room[1], 0, "counts")
+        _table(lse, True, room[0], q.shape[1], "lse")
+        _table(weights, True, room[0] * room[1], room[2], "weights")
+
+
 def _done(rc, where: str) -> bool:
     """Whether the native module made the call; raises if the library refused it."""
     if rc is NotImplemented:
@@ -537,16 +559,20 @@ def lc_append4(idx: Index, K4, V4, k_new, v_new, close_chunk: Optional[Sequence[
 
 def lc_weigh_chunks(idx: Index, q, K, chunk_ids, counts, lse, weights, stream=None) -> None:
     """Adds each listed chunk's attention weight to weights (float32 [B][H_kv][max_chunks]); lse float32 [B][H_q] as lc_sparse_decode gives it."""
-    if _done((_fast_mod or _fast()).weigh_chunks(idx.address, q, K, chunk_ids, counts, lse, weights, stream, False), "lc_weigh_chunks"):
+    room = _room(idx)
+    if _done((_fast_mod or _fast()).weigh_chunks(idx.address, q, K, chunk_ids, counts, lse, weights, stream, False, room), "lc_weigh_chunks"):
         return
+    _weigh_tables(room, q, chunk_ids, counts, lse, weights)
     _check(lib().lc_weigh_chunks(idx.handle, _ptr(q), _ptr(K), _strides3(K), _ptr(chunk_ids), _ptr(counts), chunk_ids.shape[2], q.shape[1],
                                  _ptr(lse), _ptr(weights), _stream(stream)), "lc_weigh_chunks")
 
 
 def lc_weigh_chunks4(idx: Index, q, K4, chunk_ids, counts, lse, weights, stream=None) -> None:
     """lc_weigh_chunks over a 4-bit cache."""
-    if _done((_fast_mod or _fast()).weigh_chunks(idx.address, q, K4, chunk_ids, counts, lse, weights, stream, True), "lc_weigh_chunks4"):
+    room = _room(idx)
+    if _done((_fast_mod or _fast()).weigh_chunks(idx.address, q, K4, chunk_ids, counts, lse, weights, stream, True, room), "lc_weigh_chunks4"):
         return
+    _weigh_tables(room, q, chunk_ids, counts, lse, weights)
     _check(lib().lc_weigh_chunks4(idx.handle, _ptr(q), _ptr(K4), _strides4(K4), _ptr(chunk_ids), _ptr(counts), chunk_ids.shape[2], q.shape[1],
                                   _ptr(lse), _ptr(weights), _stream(stream)), "lc_weigh_chunks4")
 
@@ -554,9 +580,14 @@ def lc_weigh_chunks4(idx: Index, q, K4, chunk_ids, counts, lse, weights, stream=
 def lc_evict_select(idx: Index, weights, keep_tokens: int, recent_tokens: int, keep_ids, keep_bounds, keep_counts, ws, keep_lens=None,
                     stream=None) -> None:
     """keep_ids int32 [B][max_chunks], keep_bounds int32 [B][max_chunks + 1], keep_counts int32 [B], keep_lens int32 [B] or None."""
-    if _done((_fast_mod or _fast()).evict_select(idx.address, weights, keep_tokens, recent_tokens, keep_ids, keep_bounds, keep_counts, ws, keep_lens, stream),
+    room = _room(idx)
+    if _done((_fast_mod or _fast()).evict_select(idx.address, weights, keep_tokens, recent_tokens, keep_ids, keep_bounds, keep_counts, ws, keep_lens, stream, room),
              "lc_evict_select"):
         return
+    _keep_tables(room, keep_ids, keep_bounds, keep_counts)
+    if room:
+        _table(weights, True, room[0] * room[1], room[2], "weights")
+        _table(keep_lens, False, room[0], 0, "keep_lens")
     _check(lib().lc_evict_select(idx.handle, _ptr(weights), int(keep_tokens), int(recent_tokens), _ptr(keep_ids), _ptr(keep_bounds),
                                  _ptr(keep_counts), _ptr(keep_lens), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)), "lc_evict_select")
 
@@ -571,6 +602,10 @@ def lc_evict_rows(idx: Index, keep_ids, keep_bounds, keep_counts, K, V, K_to, V_
     assert K.shape[:2] == K_to.shape[:2] and K.shape[3] == K_to.shape[3] and (K.element_size() == 1 or K.shape[3] == LC_HEAD_DIM), "K_to must have K's sequences, heads and row"
     assert K_to.shape[2] >= (room[3] if room else K.shape[2]) and (room is None or (K.shape[0] >= room[0] and K.shape[1] >= room[1])), \
         "K_to and V_to must have room for the index's max_tokens rows"
+    _keep_tables(room, keep_ids, keep_bounds, keep_counts)
+    if room:
+        _table(weights, True, room[0] * room[1], room[2], "weights")
+        _table(weights_to, True, room[0] * room[1], room[2], "weights_to")
     assert K.element_size() in (1, 2) and all(t.element_size() == K.element_size() for t in (V, K_to, V_to)), "caches must be all bfloat16 or all of 4 bits"
     call, strides = (lib().lc_evict_rows4, _strides4) if K.element_size() == 1 else (lib().lc_evict_rows, _strides3)
     _check(call(idx.handle, _ptr(keep_ids), _ptr(keep_bounds), _ptr(keep_counts), _ptr(K), _ptr(V), strides(K), _ptr(K_to), _ptr(V_to),

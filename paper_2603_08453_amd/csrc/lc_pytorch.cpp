@@ -417,16 +417,38 @@ PyObject* append4(PyObject*, PyObject* const* args, Py_ssize_t n) {
     });
 }
 
-// weigh_chunks(handle, q, K or K4, chunk_ids, counts, lse, weights, stream, in 4 bits)
+// Whether t, if there is one, holds `rows` rows of `row` 32-bit numbers one behind the other (row 0: that many numbers, whatever its shape).
+bool table(const at::Tensor* t, bool floats, int64_t rows, int64_t row, const char* name) {
+    if (!t || (t->is_contiguous() && t->element_size() == 4 && t->is_floating_point() == floats && t->numel() >= rows * (row ? row : 1) &&
+               (row == 0 || t->dim() < 2 || t->size(-1) == row)))
+        return true;
+    PyErr_Format(PyExc_AssertionError, "%s must be a contiguous %s table with the index's room", name, floats ? "float32" : "int32");
+    return false;
+}
+
+// The lists of the chunks that stay.
+bool keep_tables(const Room& room, const at::Tensor* ids, const at::Tensor* bounds, const at::Tensor* counts) {
+    return !room.known || (table(ids, false, room.B(), room.chunks(), "keep_ids") && table(bounds, false, room.B(), room.chunks() + 1, "keep_bounds") &&
+                           table(counts, false, room.B(), 0, "keep_counts"));
+}
+
+// weigh_chunks(handle, q, K or K4, chunk_ids, counts, lse, weights, stream, in 4 bits, room)
 PyObject* weigh_chunks(PyObject*, PyObject* const* args, Py_ssize_t n) {
     Args a(args, n);
-    if (!a.count(9)) return nullptr;
+    if (!a.count(10)) return nullptr;
     return guarded(a, [&](int* rc) {
-        const at::Tensor *q = a.tensor(1), *K = a.tensor(2), *ids = a.tensor(3);
+        const at::Tensor *q = a.tensor(1), *K = a.tensor(2), *ids = a.tensor(3), *n_t = a.tensor(4), *lse_t = a.tensor(5), *w_t = a.tensor(6);
         const bool in4 = a[8] == Py_True;
         if (!q || !K || !ids || a.foreign()) return false;
         int64_t s[3];
         if (in4 ? !cache4_strides(*K, *K, s) : !cache_strides(*K, *K, false, s)) return true;
+        const Room room = a.room(9);
+        if (room.known) {
+            const int64_t pairs = room.B() * room.H();
+            if (!table(ids, false, pairs, ids->size(-1), "chunk_ids") || !table(n_t, false, pairs, 0, "counts") ||
+                !table(lse_t, true, room.B(), q->size(1), "lse") || !table(w_t, true, pairs, room.chunks(), "weights"))
+                return true;
+        }
         const int32_t* const counts = static_cast<const int32_t*>(a.ptr(4));
         const float* const lse = static_cast<const float*>(a.ptr(5));
         float* const weights = static_cast<float*>(a.ptr(6));
@@ -444,13 +466,16 @@ PyObject* weigh_chunks(PyObject*, PyObject* const* args, Py_ssize_t n) {
     });
 }
 
-// evict_select(handle, weights, keep_tokens, recent_tokens, keep_ids, keep_bounds, keep_counts, ws, keep_lens, stream)
+// evict_select(handle, weights, keep_tokens, recent_tokens, keep_ids, keep_bounds, keep_counts, ws, keep_lens, stream, room)
 PyObject* evict_select(PyObject*, PyObject* const* args, Py_ssize_t n) {
     Args a(args, n);
-    if (!a.count(10)) return nullptr;
+    if (!a.count(11)) return nullptr;
     return guarded(a, [&](int* rc) {
-        const at::Tensor *w = a.tensor(1), *ws = a.tensor(7);
+        const at::Tensor *w = a.tensor(1), *ids_t = a.tensor(4), *bounds_t = a.tensor(5), *n_t = a.tensor(6), *ws = a.tensor(7), *lens_t = a.tensor(8);
         if (!w || !ws || a.foreign()) return false;
+        const Room room = a.room(10);
+        if (!keep_tables(room, ids_t, bounds_t, n_t)) return true;
+        if (room.known && (!table(w, true, room.B() * room.H(), room.chunks(), "weights") || !table(lens_t, false, room.B(), 0, "keep_lens"))) return true;
         const int keep = a.integer(2), recent = a.integer(3);
         if (PyErr_Occurred()) return false;
         int32_t* const ids = static_cast<int32_t*>(a.ptr(4));
@@ -494,7 +519,11 @@ PyObject* evict_rows(PyObject*, PyObject* const* args, Py_ssize_t n) {
             if (t->element_size() != (in4 ? 1 : 2)) return false;
         if (in4 ? !cache4_strides(*K, *V, s) || !cache4_strides(*K_to, *V_to, st_to) : !cache_strides(*K, *V, true, s) || !cache_strides(*K_to, *V_to, true, st_to))
             return true;
-        if (!holds_rows(*K, *K_to, a.room(11), in4)) return true;
+        const at::Tensor *ids_t = a.tensor(1), *bounds_t = a.tensor(2), *n_t = a.tensor(3), *w_t = a.tensor(8), *w_to_t = a.tensor(9);
+        const Room room = a.room(11);
+        if (!holds_rows(*K, *K_to, room, in4) || !keep_tables(room, ids_t, bounds_t, n_t)) return true;
+        const int64_t pairs = room.B() * room.H();
+        if (room.known && (!table(w_t, true, pairs, room.chunks(), "weights") || !table(w_to_t, true, pairs, room.chunks(), "weights_to"))) return true;
         const int32_t* const ids = static_cast<const int32_t*>(a.ptr(1));
         const int32_t* const bounds = static_cast<const int32_t*>(a.ptr(2));
         const int32_t* const counts = static_cast<const int32_t*>(a.ptr(3));

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_2603_08453_amd import binding as lc
-from tests.test_binding_args4 import B, H, M, T, Index, Stream, seen, t  # noqa: F401  (fixtures)
+from tests.test_binding_args4 import B, G, H, M, T, Index, Stream, seen, t  # noqa: F401  (fixtures)
 
 
 class Sized(Index):
@@ -58,3 +58,41 @@ def test_values_smaller_than_their_keys(seen, t):  # noqa: F811
         with pytest.raises(AssertionError):
             call()
     assert seen == []
+
+
+# ------------------------------------------------------------------ tables that go by the index's room for chunks
+
+def test_lists_and_weights_sized_by_the_chunks_there_are(seen, t):  # noqa: F811
+    """The index has room for M chunks; tensors made for fewer would be written behind their ends."""
+    f, i32 = (lambda *n: torch.zeros(*n)), (lambda *n: torch.zeros(*n, dtype=torch.int32))
+    select = lambda **kw: lc.lc_evict_select(Sized, *(kw.get(k, t[k]) for k in ("weights",)), 10, 0, *(kw.get(k, t[k]) for k in ("keep", "bounds", "n")), t["ws"],
+                                             keep_lens=kw.get("lens", t["lens"]), stream=Stream)
+    for bad in (dict(weights=f(B, H, M - 1)), dict(weights=f(B, H - 1, M)), dict(weights=f(B, H, M + 1)), dict(weights=f(B, H, M).half()), dict(weights=f(B, M, H).transpose(1, 2)),
+                dict(keep=i32(B, M - 1)), dict(keep=i32(B - 1, M)), dict(keep=i32(B, M + 1)), dict(keep=i32(B, M).long()), dict(keep=i32(M, B).t()),
+                dict(bounds=i32(B, M)), dict(bounds=i32(B - 1, M + 1)), dict(bounds=i32(B, M + 1).short()), dict(n=i32(B - 1)), dict(n=i32(2 * B)[::2]), dict(lens=i32(B - 1))):
+        with pytest.raises(AssertionError):
+            select(**bad)
+    rows = lambda **kw: lc.lc_evict_rows(Sized, *(kw.get(k, t[k]) for k in ("keep", "bounds", "n")), t["K"], t["V"], t["Kb"], t["Vb"],
+                                         **{k: kw.get(k, t[k]) for k in ("weights", "weights_to")}, stream=Stream)
+    for bad in (dict(weights=f(B, H, M - 1)), dict(weights_to=f(B, H, M - 1)), dict(weights_to=f(B, H - 1, M)), dict(weights_to=f(B, M, H).transpose(1, 2)),
+                dict(keep=i32(B, M - 1)), dict(bounds=i32(B, M)), dict(n=i32(B - 1))):
+        with pytest.raises(AssertionError):
+            rows(**bad)
+    for call, K in ((lc.lc_weigh_chunks, t["K"]), (lc.lc_weigh_chunks4, t["K4"])):
+        for bad in (dict(weights=f(B, H, M - 1)), dict(weights=f(B, H, M + 1)), dict(weights=f(B - 1, H, M)), dict(weights=f(B, H, M).double()), dict(lse=f(B, H * G - 1)),
+                    dict(lse=f(H * G, B).t()), dict(counts=i32(B, H - 1)), dict(counts=i32(B, H).long()), dict(ids=i32(B, H - 1, M)), dict(ids=i32(B, H, 2 * M)[:, :, ::2])):
+            with pytest.raises(AssertionError):
+                call(Sized, t["q"], K, *(bad.get(k, t[k]) for k in ("ids", "counts", "lse", "weights")), stream=Stream)
+    assert seen == []
+
+
+def test_tables_that_have_the_room(seen, t):  # noqa: F811
+    """Flat ones, and ones with room for more sequences, as before."""
+    more = torch.zeros(B + 1, H, M)
+    lc.lc_evict_select(Sized, more, 10, 0, t["keep"].reshape(-1), t["bounds"], t["n"].reshape(B, 1), t["ws"], stream=Stream)
+    lc.lc_evict_rows(Sized, t["keep"], t["bounds"], t["n"], t["K"], t["V"], t["Kb"], t["Vb"], weights=more, weights_to=t["weights_to"].reshape(-1), stream=Stream)
+    lc.lc_evict_rows(Sized, t["keep"], t["bounds"], t["n"], t["K"], t["V"], t["Kb"], t["Vb"], stream=Stream)
+    lc.lc_weigh_chunks(Sized, t["q"], t["K"], t["ids"], t["counts"], t["lse"].reshape(-1), more, stream=Stream)
+    # a list's table may have less or more room than the index
+    lc.lc_weigh_chunks4(Sized, t["q"], t["K4"], torch.zeros(B, H, 2, dtype=torch.int32), t["counts"], t["lse"], t["weights"], stream=Stream)
+    assert [name for name, _ in seen] == ["evict_select", "evict_rows", "evict_rows", "weigh_chunks", "weigh_chunks4"]
