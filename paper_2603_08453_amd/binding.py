@@ -469,6 +469,11 @@ def _strides4(t) -> "ctypes.Array":
     return (ctypes.c_int64 * 3)(t.stride(0), t.stride(1), t.stride(2))
 
 
+def _bfloat16s(*tensors) -> None:
+    """The tensors hold bfloat16 values, or their bits in an integer type."""
+    assert all(t.element_size() == 2 and str(t.dtype) != "torch.float16" for t in tensors), "queries, keys and values must be bfloat16"
+
+
 def _cache4(K4, V4) -> None:
     assert K4.shape == V4.shape and K4.stride() == V4.stride() and V4.element_size() == 1, "K4 and V4 must be of the same type, shape and strides"
 
@@ -514,7 +519,8 @@ def _move4(call, where, K, V, K4, V4, first, counts, stream, store):
         return
     B, H_kv, rows, d = K.shape
     assert K.shape == V.shape and K.stride() == V.stride() and K4.shape == V4.shape and K4.stride() == V4.stride()
-    assert K4.shape[:2] == K.shape[:2] and K.element_size() == V.element_size() == 2 and V4.element_size() == 1
+    _bfloat16s(K, V)
+    assert K4.shape[:2] == K.shape[:2] and V4.element_size() == 1
     counts = [rows] * B if counts is None else [int(n) for n in counts]
     first = None if first is None else [int(n) for n in first]
     assert len(counts) == B and max(counts, default=0) <= rows and (first is None or len(first) == B)
@@ -538,6 +544,7 @@ def lc_sparse_decode4(idx: Index, q, K4, V4, chunk_ids, counts, out, ws, lse=Non
     """lc_sparse_decode over a 4-bit cache (uint8 [B][H_kv][tokens][68])."""
     if _done((_fast_mod or _fast()).sparse_decode4(idx.address, q, K4, V4, chunk_ids, counts, out, ws, lse, stream), "lc_sparse_decode4"):
         return
+    _bfloat16s(q)
     _cache4(K4, V4)
     _check(lib().lc_sparse_decode4(idx.handle, _ptr(q), _ptr(K4), _ptr(V4), _strides4(K4), _ptr(chunk_ids), _ptr(counts),
                                    chunk_ids.shape[2], q.shape[1], _ptr(out), _ptr(lse), _ptr(ws), ws.numel() * ws.element_size(),
@@ -551,6 +558,7 @@ def lc_append4(idx: Index, K4, V4, k_new, v_new, close_chunk: Optional[Sequence[
     cc = None
     if close_chunk is not None:
         cc = (ctypes.c_uint8 * len(close_chunk))(*[1 if c else 0 for c in close_chunk])
+    _bfloat16s(k_new, v_new)
     _cache4(K4, V4)
     _check(lib().lc_append4(idx.handle, _ptr(K4), _ptr(V4), _strides4(K4), _ptr(k_new), _ptr(v_new), cc, _stream(stream)), "lc_append4")
 
@@ -562,6 +570,7 @@ def lc_weigh_chunks(idx: Index, q, K, chunk_ids, counts, lse, weights, stream=No
     room = _room(idx)
     if _done((_fast_mod or _fast()).weigh_chunks(idx.address, q, K, chunk_ids, counts, lse, weights, stream, False, room), "lc_weigh_chunks"):
         return
+    _bfloat16s(q, K)
     _weigh_tables(room, q, chunk_ids, counts, lse, weights)
     _check(lib().lc_weigh_chunks(idx.handle, _ptr(q), _ptr(K), _strides3(K), _ptr(chunk_ids), _ptr(counts), chunk_ids.shape[2], q.shape[1],
                                  _ptr(lse), _ptr(weights), _stream(stream)), "lc_weigh_chunks")
@@ -572,6 +581,7 @@ def lc_weigh_chunks4(idx: Index, q, K4, chunk_ids, counts, lse, weights, stream=
     room = _room(idx)
     if _done((_fast_mod or _fast()).weigh_chunks(idx.address, q, K4, chunk_ids, counts, lse, weights, stream, True, room), "lc_weigh_chunks4"):
         return
+    _bfloat16s(q)
     _weigh_tables(room, q, chunk_ids, counts, lse, weights)
     _check(lib().lc_weigh_chunks4(idx.handle, _ptr(q), _ptr(K4), _strides4(K4), _ptr(chunk_ids), _ptr(counts), chunk_ids.shape[2], q.shape[1],
                                   _ptr(lse), _ptr(weights), _stream(stream)), "lc_weigh_chunks4")

@@ -11,6 +11,7 @@
 #include <c10/hip/HIPStream.h>
 
 #include <exception>
+#include <initializer_list>
 
 #include "lychee.h"
 
@@ -300,6 +301,16 @@ PyObject* append(PyObject*, PyObject* const* args, Py_ssize_t n) {
     });
 }
 
+// Whether the tensors hold bfloat16 values, or their bits in an integer type.
+bool bfloat16s(std::initializer_list<const at::Tensor*> tensors) {
+    for (const at::Tensor* t : tensors)
+        if (t->element_size() != 2 || t->scalar_type() == at::kHalf) {
+            PyErr_SetString(PyExc_AssertionError, "queries, keys and values must be bfloat16");
+            return false;
+        }
+    return true;
+}
+
 // Strides of a 4-bit cache, in bytes.
 bool cache4_strides(const at::Tensor& K4, const at::Tensor& V4, int64_t (&s)[3]) {
     if (!K4.sizes().equals(V4.sizes()) || !K4.strides().equals(V4.strides())) {
@@ -341,6 +352,7 @@ PyObject* move4(PyObject*, PyObject* const* args, Py_ssize_t n) {
         if (K->dim() != 4 || K4->dim() != 4 || K->element_size() != 2 || V->element_size() != 2 || !K->sizes().equals(V->sizes()) || !K4->sizes().equals(V4->sizes()) ||
             K->size(0) != K4->size(0) || K->size(1) != K4->size(1) || K->size(0) > 256 || K->size(2) > 0x7fffffffL || K4->size(2) > 0x7fffffffL)
             return false;
+        if (!bfloat16s({K, V})) return true;
         int64_t s[3], s4[3];
         if (!cache_strides(*K, *V, true, s) || !cache4_strides(*K4, *V4, s4)) return true;
         const int B = (int)K->size(0), H = (int)K->size(1), rows = (int)K->size(2), d = (int)K->size(3);
@@ -373,7 +385,7 @@ PyObject* sparse_decode4(PyObject*, PyObject* const* args, Py_ssize_t n) {
         const at::Tensor *q = a.tensor(1), *K = a.tensor(2), *V = a.tensor(3), *ids = a.tensor(4), *ws = a.tensor(7);
         if (!q || !K || !V || !ids || !ws || a.foreign()) return false;
         int64_t s[3];
-        if (!cache4_strides(*K, *V, s)) return true;
+        if (!bfloat16s({q}) || !cache4_strides(*K, *V, s)) return true;
         const int32_t* const counts = static_cast<const int32_t*>(a.ptr(5));
         float* const out = static_cast<float*>(a.ptr(6));
         float* const lse = static_cast<float*>(a.ptr(8));
@@ -401,7 +413,7 @@ PyObject* append4(PyObject*, PyObject* const* args, Py_ssize_t n) {
         const at::Tensor *K = a.tensor(1), *V = a.tensor(2), *k = a.tensor(3), *v = a.tensor(4);
         if (!K || !V || !k || !v || a.foreign()) return false;
         int64_t s[3];
-        if (!cache4_strides(*K, *V, s)) return true;
+        if (!bfloat16s({k, v}) || !cache4_strides(*K, *V, s)) return true;
         uint8_t flags[1024] = {};                            // lc_append4 takes at most 1024 sequences
         const bool given = a[5] != Py_None;
         if (given && !close_flags(a[5], flags)) return false;
@@ -441,7 +453,7 @@ PyObject* weigh_chunks(PyObject*, PyObject* const* args, Py_ssize_t n) {
         const bool in4 = a[8] == Py_True;
         if (!q || !K || !ids || a.foreign()) return false;
         int64_t s[3];
-        if (in4 ? !cache4_strides(*K, *K, s) : !cache_strides(*K, *K, false, s)) return true;
+        if (!bfloat16s({q}) || (in4 ? !cache4_strides(*K, *K, s) : !bfloat16s({K}) || !cache_strides(*K, *K, false, s))) return true;
         const Room room = a.room(9);
         if (room.known) {
             const int64_t pairs = room.B() * room.H();

@@ -96,3 +96,31 @@ def test_tables_that_have_the_room(seen, t):  # noqa: F811
     # a list's table may have less or more room than the index
     lc.lc_weigh_chunks4(Sized, t["q"], t["K4"], torch.zeros(B, H, 2, dtype=torch.int32), t["counts"], t["lse"], t["weights"], stream=Stream)
     assert [name for name, _ in seen] == ["evict_select", "evict_rows", "evict_rows", "weigh_chunks", "weigh_chunks4"]
+
+
+# ------------------------------------------------------------------ types
+
+def test_other_types_than_bfloat16(seen, t):  # noqa: F811
+    """float16 has as many bytes: its bits would be taken for bfloat16's."""
+    half = {k: t[k].half() for k in ("q", "K", "V", "row")}
+    wide = {k: t[k].float() for k in ("q", "row")}
+    for call in (lambda: lc.lc_cache4_store(half["K"], half["V"], t["K4"], t["V4"], stream=Stream),
+                 lambda: lc.lc_cache4_store(t["K"], half["V"], t["K4"], t["V4"], stream=Stream),
+                 lambda: lc.lc_cache4_load(t["K4"], t["V4"], half["K"], half["V"], stream=Stream),
+                 lambda: lc.lc_sparse_decode4(Index, half["q"], t["K4"], t["V4"], t["ids"], t["counts"], t["out"], t["ws"], stream=Stream),
+                 lambda: lc.lc_sparse_decode4(Index, wide["q"], t["K4"], t["V4"], t["ids"], t["counts"], t["out"], t["ws"], stream=Stream),
+                 lambda: lc.lc_append4(Index, t["K4"], t["V4"], half["row"], t["row"], stream=Stream),
+                 lambda: lc.lc_append4(Index, t["K4"], t["V4"], t["row"], wide["row"], stream=Stream),
+                 lambda: lc.lc_weigh_chunks(Index, t["q"], half["K"], t["ids"], t["counts"], t["lse"], t["weights"], stream=Stream),
+                 lambda: lc.lc_weigh_chunks(Index, half["q"], t["K"], t["ids"], t["counts"], t["lse"], t["weights"], stream=Stream),
+                 lambda: lc.lc_weigh_chunks4(Index, wide["q"], t["K4"], t["ids"], t["counts"], t["lse"], t["weights"], stream=Stream)):
+        with pytest.raises(AssertionError):
+            call()
+    assert seen == []
+    # bfloat16 bits in another type's clothes are bfloat16 bits
+    bits = {k: t[k].view(torch.int16) for k in ("q", "K", "V", "row")}
+    lc.lc_cache4_store(bits["K"], bits["V"], t["K4"], t["V4"], stream=Stream)
+    lc.lc_sparse_decode4(Index, bits["q"], t["K4"], t["V4"], t["ids"], t["counts"], t["out"], t["ws"], stream=Stream)
+    lc.lc_append4(Index, t["K4"], t["V4"], bits["row"], bits["row"], stream=Stream)
+    lc.lc_weigh_chunks(Index, bits["q"], bits["K"], t["ids"], t["counts"], t["lse"], t["weights"], stream=Stream)
+    assert [name for name, _ in seen] == ["cache4_store", "sparse_decode4", "append4", "weigh_chunks"]
