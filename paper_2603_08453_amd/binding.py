@@ -490,6 +490,15 @@ def _table(t, floats: bool, rows: int, row: int, name: str) -> None:
         f"{name} must be a contiguous {'float32' if floats else 'int32'} table with the index's room"
 
 
+def _dense(t, n: int, name: str) -> None:
+    assert t.is_contiguous() and t.numel() >= n, f"{name} must be contiguous and hold the index's sequences and heads"
+
+
+def _holds(room, K, rows: int) -> None:
+    assert K.shape[0] >= room[0] and K.shape[1] >= room[1] and K.shape[2] >= rows, \
+        "the cache must have the index's sequences and heads, and max_tokens rows where it is appended to"
+
+
 def _keep_tables(room, keep_ids, keep_bounds, keep_counts) -> None:
     if room:
         _table(keep_ids, False, room[0], room[2], "keep_ids")
@@ -497,12 +506,13 @@ def _keep_tables(room, keep_ids, keep_bounds, keep_counts) -> None:
         _table(keep_counts, False, room[0], 0, "keep_counts")
 
 
-def _weigh_tables(room, q, chunk_ids, counts, lse, weights) -> None:
+def _list_tables(room, q, K, chunk_ids, counts, lse) -> None:
     if room:
+        _dense(q, room[0] * q.shape[1] * LC_HEAD_DIM, "q")
+        _holds(room, K, 0)
         _table(chunk_ids, False, room[0] * room[1], chunk_ids.shape[-1], "chunk_ids")
         _table(counts, False, room[0] * room[1], 0, "counts")
         _table(lse, True, room[0], q.shape[1], "lse")
-        _table(weights, True, room[0] * room[1], room[2], "weights")
 
 
 def _done(rc, where: str) -> bool:
@@ -542,10 +552,14 @@ def lc_cache4_load(K4, V4, K, V, first=None, counts=None, stream=None) -> None:
 
 def lc_sparse_decode4(idx: Index, q, K4, V4, chunk_ids, counts, out, ws, lse=None, stream=None) -> None:
     """lc_sparse_decode over a 4-bit cache (uint8 [B][H_kv][tokens][68])."""
-    if _done((_fast_mod or _fast()).sparse_decode4(idx.address, q, K4, V4, chunk_ids, counts, out, ws, lse, stream), "lc_sparse_decode4"):
+    room = _room(idx)
+    if _done((_fast_mod or _fast()).sparse_decode4(idx.address, q, K4, V4, chunk_ids, counts, out, ws, lse, stream, room), "lc_sparse_decode4"):
         return
     _bfloat16s(q)
     _cache4(K4, V4)
+    _list_tables(room, q, K4, chunk_ids, counts, lse)
+    if room:
+        _table(out, True, room[0] * q.shape[1] * LC_HEAD_DIM, 0, "out")
     _check(lib().lc_sparse_decode4(idx.handle, _ptr(q), _ptr(K4), _ptr(V4), _strides4(K4), _ptr(chunk_ids), _ptr(counts),
                                    chunk_ids.shape[2], q.shape[1], _ptr(out), _ptr(lse), _ptr(ws), ws.numel() * ws.element_size(),
                                    _stream(stream)), "lc_sparse_decode4")
@@ -553,13 +567,18 @@ def lc_sparse_decode4(idx: Index, q, K4, V4, chunk_ids, counts, out, ws, lse=Non
 
 def lc_append4(idx: Index, K4, V4, k_new, v_new, close_chunk: Optional[Sequence[int]] = None, stream=None) -> None:
     """lc_append over a 4-bit cache."""
-    if _done((_fast_mod or _fast()).append4(idx.address, K4, V4, k_new, v_new, close_chunk, stream), "lc_append4"):
+    room = _room(idx)
+    if _done((_fast_mod or _fast()).append4(idx.address, K4, V4, k_new, v_new, close_chunk, stream, room), "lc_append4"):
         return
     cc = None
     if close_chunk is not None:
         cc = (ctypes.c_uint8 * len(close_chunk))(*[1 if c else 0 for c in close_chunk])
     _bfloat16s(k_new, v_new)
     _cache4(K4, V4)
+    if room:
+        _holds(room, K4, room[3])
+        _dense(k_new, room[0] * room[1] * LC_HEAD_DIM, "k_new")
+        _dense(v_new, room[0] * room[1] * LC_HEAD_DIM, "v_new")
     _check(lib().lc_append4(idx.handle, _ptr(K4), _ptr(V4), _strides4(K4), _ptr(k_new), _ptr(v_new), cc, _stream(stream)), "lc_append4")
 
 
@@ -571,7 +590,9 @@ def lc_weigh_chunks(idx: Index, q, K, chunk_ids, counts, lse, weights, stream=No
     if _done((_fast_mod or _fast()).weigh_chunks(idx.address, q, K, chunk_ids, counts, lse, weights, stream, False, room), "lc_weigh_chunks"):
         return
     _bfloat16s(q, K)
-    _weigh_tables(room, q, chunk_ids, counts, lse, weights)
+    _list_tables(room, q, K, chunk_ids, counts, lse)
+    if room:
+        _table(weights, True, room[0] * room[1], room[2], "weights")
     _check(lib().lc_weigh_chunks(idx.handle, _ptr(q), _ptr(K), _strides3(K), _ptr(chunk_ids), _ptr(counts), chunk_ids.shape[2], q.shape[1],
                                  _ptr(lse), _ptr(weights), _stream(stream)), "lc_weigh_chunks")
 
@@ -582,7 +603,9 @@ def lc_weigh_chunks4(idx: Index, q, K4, chunk_ids, counts, lse, weights, stream=
     if _done((_fast_mod or _fast()).weigh_chunks(idx.address, q, K4, chunk_ids, counts, lse, weights, stream, True, room), "lc_weigh_chunks4"):
         return
     _bfloat16s(q)
-    _weigh_tables(room, q, chunk_ids, counts, lse, weights)
+    _list_tables(room, q, K4, chunk_ids, counts, lse)
+    if room:
+        _table(weights, True, room[0] * room[1], room[2], "weights")
     _check(lib().lc_weigh_chunks4(idx.handle, _ptr(q), _ptr(K4), _strides4(K4), _ptr(chunk_ids), _ptr(counts), chunk_ids.shape[2], q.shape[1],
                                   _ptr(lse), _ptr(weights), _stream(stream)), "lc_weigh_chunks4")
 

@@ -377,15 +377,45 @@ PyObject* move4(PyObject*, PyObject* const* args, Py_ssize_t n) {
     });
 }
 
-// sparse_decode4(handle, q, K4, V4, chunk_ids, counts, out, ws, lse, stream)
+// Whether t, if there is one, holds `rows` rows of `row` 32-bit numbers one behind the other (row 0: that many numbers, whatever its shape).
+bool table(const at::Tensor* t, bool floats, int64_t rows, int64_t row, const char* name) {
+    if (!t || (t->is_contiguous() && t->element_size() == 4 && t->is_floating_point() == floats && t->numel() >= rows * (row ? row : 1) &&
+               (row == 0 || t->dim() < 2 || t->size(-1) == row)))
+        return true;
+    PyErr_Format(PyExc_AssertionError, "%s must be a contiguous %s table with the index's room", name, floats ? "float32" : "int32");
+    return false;
+}
+
+// Whether an input holds n values one behind the other.
+bool dense(const at::Tensor& t, int64_t n, const char* name) {
+    if (t.is_contiguous() && t.numel() >= n) return true;
+    PyErr_Format(PyExc_AssertionError, "%s must be contiguous and hold the index's sequences and heads", name);
+    return false;
+}
+// Whether a cache (of four dimensions) has the index's sequences and heads, and `rows` rows.
+bool holds(const at::Tensor& K, const Room& room, int64_t rows) {
+    if (K.size(0) >= room.B() && K.size(1) >= room.H() && K.size(2) >= rows) return true;
+    PyErr_SetString(PyExc_AssertionError, "the cache must have the index's sequences and heads, and max_tokens rows where it is appended to");
+    return false;
+}
+
+// sparse_decode4(handle, q, K4, V4, chunk_ids, counts, out, ws, lse, stream, room)
 PyObject* sparse_decode4(PyObject*, PyObject* const* args, Py_ssize_t n) {
     Args a(args, n);
-    if (!a.count(10)) return nullptr;
+    if (!a.count(11)) return nullptr;
     return guarded(a, [&](int* rc) {
         const at::Tensor *q = a.tensor(1), *K = a.tensor(2), *V = a.tensor(3), *ids = a.tensor(4), *ws = a.tensor(7);
         if (!q || !K || !V || !ids || !ws || a.foreign()) return false;
         int64_t s[3];
         if (!bfloat16s({q}) || !cache4_strides(*K, *V, s)) return true;
+        const at::Tensor *n_t = a.tensor(5), *out_t = a.tensor(6), *lse_t = a.tensor(8);
+        const Room room = a.room(10);
+        if (room.known) {
+            const int64_t pairs = room.B() * room.H(), values = room.B() * q->size(1) * LC_HEAD_DIM;
+            if (!dense(*q, values, "q") || !holds(*K, room, 0) || !table(ids, false, pairs, ids->size(-1), "chunk_ids") || !table(n_t, false, pairs, 0, "counts") ||
+                !table(out_t, true, values, 0, "out") || !table(lse_t, true, room.B(), q->size(1), "lse"))
+                return true;
+        }
         const int32_t* const counts = static_cast<const int32_t*>(a.ptr(5));
         float* const out = static_cast<float*>(a.ptr(6));
         float* const lse = static_cast<float*>(a.ptr(8));
@@ -405,15 +435,20 @@ PyObject* sparse_decode4(PyObject*, PyObject* const* args, Py_ssize_t n) {
     });
 }
 
-// append4(handle, K4, V4, k_new, v_new, close flags or None, stream)
+// append4(handle, K4, V4, k_new, v_new, close flags or None, stream, room)
 PyObject* append4(PyObject*, PyObject* const* args, Py_ssize_t n) {
     Args a(args, n);
-    if (!a.count(7)) return nullptr;
+    if (!a.count(8)) return nullptr;
     return guarded(a, [&](int* rc) {
         const at::Tensor *K = a.tensor(1), *V = a.tensor(2), *k = a.tensor(3), *v = a.tensor(4);
         if (!K || !V || !k || !v || a.foreign()) return false;
         int64_t s[3];
         if (!bfloat16s({k, v}) || !cache4_strides(*K, *V, s)) return true;
+        const Room room = a.room(7);
+        if (room.known) {
+            const int64_t values = room.B() * room.H() * LC_HEAD_DIM;
+            if (!holds(*K, room, room.tokens()) || !dense(*k, values, "k_new") || !dense(*v, values, "v_new")) return true;
+        }
         uint8_t flags[1024] = {};                            // lc_append4 takes at most 1024 sequences
         const bool given = a[5] != Py_None;
         if (given && !close_flags(a[5], flags)) return false;
@@ -427,15 +462,6 @@ PyObject* append4(PyObject*, PyObject* const* args, Py_ssize_t n) {
         *rc = g_append4(idx, kd, vd, s, kn, vn, given ? flags : nullptr, st);
         return true;
     });
-}
-
-// Whether t, if there is one, holds `rows` rows of `row` 32-bit numbers one behind the other (row 0: that many numbers, whatever its shape).
-bool table(const at::Tensor* t, bool floats, int64_t rows, int64_t row, const char* name) {
-    if (!t || (t->is_contiguous() && t->element_size() == 4 && t->is_floating_point() == floats && t->numel() >= rows * (row ? row : 1) &&
-               (row == 0 || t->dim() < 2 || t->size(-1) == row)))
-        return true;
-    PyErr_Format(PyExc_AssertionError, "%s must be a contiguous %s table with the index's room", name, floats ? "float32" : "int32");
-    return false;
 }
 
 // The lists of the chunks that stay.
@@ -457,8 +483,8 @@ PyObject* weigh_chunks(PyObject*, PyObject* const* args, Py_ssize_t n) {
         const Room room = a.room(9);
         if (room.known) {
             const int64_t pairs = room.B() * room.H();
-            if (!table(ids, false, pairs, ids->size(-1), "chunk_ids") || !table(n_t, false, pairs, 0, "counts") ||
-                !table(lse_t, true, room.B(), q->size(1), "lse") || !table(w_t, true, pairs, room.chunks(), "weights"))
+            if (!dense(*q, room.B() * q->size(1) * LC_HEAD_DIM, "q") || !holds(*K, room, 0) ||
+                !table(ids, false, pairs, ids->size(-1), "chunk_ids") || !table(n_t, false, pairs, 0, "counts") || !table(lse_t, true, room.B(), q->size(1), "lse") || !table(w_t, true, pairs, room.chunks(), "weights"))
                 return true;
         }
         const int32_t* const counts = static_cast<const int32_t*>(a.ptr(4));

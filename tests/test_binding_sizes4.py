@@ -124,3 +124,38 @@ def test_other_types_than_bfloat16(seen, t):  # noqa: F811
     lc.lc_append4(Index, t["K4"], t["V4"], bits["row"], bits["row"], stream=Stream)
     lc.lc_weigh_chunks(Index, bits["q"], bits["K"], t["ids"], t["counts"], t["lse"], t["weights"], stream=Stream)
     assert [name for name, _ in seen] == ["cache4_store", "sparse_decode4", "append4", "weigh_chunks"]
+
+
+# ------------------------------------------------------------------ attention, lazy update
+
+def test_attention_into_tensors_that_are_too_small(seen, t):  # noqa: F811
+    f, i32, bf = (lambda *n: torch.zeros(*n)), (lambda *n: torch.zeros(*n, dtype=torch.int32)), (lambda *n: torch.zeros(*n, dtype=torch.bfloat16))
+    attend = lambda **kw: lc.lc_sparse_decode4(Sized, *(kw.get(k, t[k]) for k in ("q", "K4", "V4", "ids", "counts", "out")), t["ws"], lse=kw.get("lse", t["lse"]), stream=Stream)
+    for bad in (dict(out=f(B, H * G - 1, 128)), dict(out=f(B - 1, H * G, 128)), dict(out=f(B, H * G, 128).half()), dict(out=f(B, H * G, 256)[..., ::2]), dict(lse=f(B, H * G - 1)),
+                dict(q=bf(B - 1, H * G, 128)), dict(q=bf(H * G, B, 128).transpose(0, 1)), dict(ids=i32(B, H - 1, M)), dict(ids=i32(B, H, 2 * M)[:, :, ::2]),
+                dict(counts=i32(B, H - 1)), dict(K4=_narrow(b=B - 1), V4=_narrow(b=B - 1)), dict(K4=_narrow(h=H - 1), V4=_narrow(h=H - 1))):
+        with pytest.raises(AssertionError):
+            attend(**bad)
+    for call, K in ((lc.lc_weigh_chunks, _wide), (lc.lc_weigh_chunks4, _narrow)):
+        for bad in (dict(q=bf(B - 1, H * G, 128)), dict(K=K(b=B - 1)), dict(K=K(h=H - 1))):
+            with pytest.raises(AssertionError):
+                call(Sized, bad.get("q", t["q"]), bad.get("K", K()), t["ids"], t["counts"], t["lse"], t["weights"], stream=Stream)
+    assert seen == []
+    attend(out=f(B, H * G * 128), lse=f(B * H * G), q=bf(B, H * G, 1, 128))
+    attend(K4=_narrow(rows=2), V4=_narrow(rows=2))           # (rows behind the tokens there are need not be)
+    assert [name for name, _ in seen] == ["sparse_decode4"] * 2
+
+
+def test_appending_to_a_cache_that_is_too_small(seen, t):  # noqa: F811
+    bf = lambda *n: torch.zeros(*n, dtype=torch.bfloat16)
+    append = lambda K, V, k=t["row"], v=t["row"]: lc.lc_append4(Sized, K, V, k, v, stream=Stream)
+    for short in (dict(rows=T - 1), dict(h=H - 1), dict(b=B - 1)):
+        with pytest.raises(AssertionError):
+            append(_narrow(**short), _narrow(**short))
+    for k in (bf(B, H - 1, 128), bf(B - 1, H, 128), bf(H, B, 128).transpose(0, 1), bf(B, H, 256)[..., ::2]):
+        for new in ((k, t["row"]), (t["row"], k)):
+            with pytest.raises(AssertionError):
+                append(t["K4"], t["V4"], *new)
+    assert seen == []
+    append(_narrow(rows=T), _narrow(rows=T), bf(B, 1, H, 128), bf(B, H, 1, 128))
+    assert [name for name, _ in seen] == ["append4"]
