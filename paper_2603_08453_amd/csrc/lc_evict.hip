@@ -71,7 +71,8 @@ lc_weigh_kernel(const LcWeighArgs a) {
     float* weights = a.weights + (size_t)bh * ix.cap[0];
     const int* bnd = ix.bounds + (size_t)b * (ix.cap[0] + 1);
     const float scale = 0.08838834764831845f * LC_LOG2E;
-    const float off = lse == LC_NEG_INF ? LC_NEG_INF : -lse * LC_LOG2E;      // (a head that attended to nothing adds nothing)
+    const float off = -lse * LC_LOG2E;
+    const bool counts_in = n < G && lse != LC_NEG_INF;       // (a head that attended to nothing adds nothing, whatever its logits are now)
     constexpr int ROW = IN4 ? LC_ROW4 : 2 * LC_D, HALVES = LC_WG_ROWS / 16, PIECES = IN4 ? 1 : 4;
     const int slab_bytes = (a.max_tokens - 1) * a.tok + ROW;
     const __amdgpu_buffer_rsrc_t Kr = lc_buffer(static_cast<const char*>(a.K) + (size_t)b * a.seq + (size_t)h * a.head, slab_bytes);
@@ -106,7 +107,7 @@ lc_weigh_kernel(const LcWeighArgs a) {
         return sum;
     };
     auto total = [&](float sum) LC_INLINE -> float {
-        sum = lc_sum16(n < G ? sum : 0.f);
+        sum = lc_sum16(counts_in ? sum : 0.f);
         sum = lc_add_halves(sum, sum);
         return lc_add_rows(sum, sum);
     };
