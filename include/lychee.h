@@ -376,10 +376,11 @@ int lc_append4(lc_index* idx, void* K4, void* V4, const int64_t strides4[3], con
  *
  * lc_weigh_chunks -- for every listed chunk c of (b, h)
  *   weights[b][h][c] += sum over its tokens t and the group's heads g of exp(q_g . k_t / sqrt(d) - lse_g).
- *   chunk_ids, counts, cap   as in lc_sparse_decode, ascending; an entry that is no chunk of the sequence, or no larger than the entry before it,
- *                            is passed over
+ *   chunk_ids, counts, cap   as in lc_sparse_decode, the chunks ascending.  An entry that is no chunk of the sequence is passed over (it holds no tokens in
+ *                            lc_sparse_decode4 either), and so is one no larger than a chunk right before it.  In a list that does not ascend otherwise a
+ *                            chunk that comes back further on is added to once or twice
  *   lse        float32 [B][H_q] as lc_sparse_decode or lc_decode_step gave it for the same q; a head with -inf adds nothing
- * The same bits every time; every chunk is added to once.  Chunks that are not listed, and the open tail, are not touched.
+ * The same bits every time, and every chunk added to once, for such lists.  Chunks that are not listed, and the open tail, are not touched.
  */
 int lc_weigh_chunks(const lc_index* idx, const void* q, const void* K, const int64_t k_strides[3], const int32_t* chunk_ids,
                     const int32_t* counts, int cap, int H_q, const float* lse, float* weights, void* stream);

@@ -118,8 +118,8 @@ lc_weigh_kernel(const LcWeighArgs a) {
             id = lc_buf_load_i32(ids_r, e0 + lane);
             before = lc_buf_load_i32(ids_r, max(0, e0 + lane - 1));
         }
-        // (an entry that is no chunk, or no larger than the one before it, is passed over: it has no tokens)
-        const bool real = lane < n_e && id >= 0 && id < M && (e0 + lane == 0 || id > before);
+        // (an entry that is no chunk, or no larger than a chunk right before it, is passed over: it has no tokens)
+        const bool real = lane < n_e && id >= 0 && id < M && (e0 + lane == 0 || id > before || before >= M);
         const int at = real ? id : 0;
         const int begin = bnd[at], end = real ? min(bnd[at + 1], a.max_tokens) : begin;
         const float so_far = weights[at];

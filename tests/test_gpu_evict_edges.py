@@ -48,3 +48,20 @@ def test_heads_that_attended_to_nothing_with_keys_that_are_no_numbers(C, bits, l
     got = _weigh(C, c, qb, t, n, some, before, bits)
     fine = np.delete(np.arange(M), bad)
     assert np.isnan(got[0, 0, bad[0]]) and np.isfinite(got[0, 0, fine]).all() and (got[0, 0, fine] > 2).all()
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_entries_that_are_no_chunk_between_others(C, bits):
+    """They hold no tokens, as in the attention; the chunk behind one is not measured against it."""
+    import torch
+    c = C.Cache(81, 1, 4, [400], [np.arange(0, 401, 10)])
+    M = 40
+    qb = c.query()
+    good = [0, 4, 7, 9, 20, 39]
+    lse = np.full((1, 4), 4.0, dtype=np.float32)
+    before = np.ones((1, 1, M), dtype=np.float32)
+    t, n = c.table([[np.array(good)]])
+    want = _weigh(C, c, qb, t, n, lse, before, bits)
+    holes = np.array([[[M + 5, 0, 0x7fffffff, 4, -1, 7, M, 9, -0x80000000, 20, 39, M]]], dtype=np.int32)
+    got = _weigh(C, c, qb, torch.from_numpy(holes).cuda(), torch.tensor([[12]], dtype=torch.int32, device="cuda"), lse, before, bits)
+    assert np.array_equal(got, want) and (want[0, 0, good] > 1).all() and (np.delete(want[0, 0], good) == 1).all()
