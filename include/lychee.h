@@ -343,7 +343,7 @@ int lc_append(lc_index* idx, void* K, void* V, const int64_t kv_strides[3],
  * half a step; codes are rounded to the nearest, ties to the even code.  A block with an infinity or a not-a-number
  * becomes 32 not-a-numbers; finite values stay finite (with s = 253 the code of 4 would be an infinity: 3 stands in).
  *   first    host int32[B], or NULL for zeros
- *   counts   host int32[B]; rows behind the range are left as they were
+ *   counts   host int32[B]; rows behind the range are left as they were.  Where all are 0 (K and V may be NULL then) nothing is enqueued
  *   max_tokens   rows of K4 and V4 per (sequence, head): first + count beyond it is LC_ERR_CAPACITY, nothing enqueued
  * Host arrays are read before the call returns (a captured launch keeps their values).
  */

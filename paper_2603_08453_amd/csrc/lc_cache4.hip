@@ -581,7 +581,10 @@ int check_strides16(const int64_t s[3]) {
 // Rows of all sequences of a store or load, LC_C4_BATCH sequences to a launch.
 int move_rows(bool store, const void* K, const void* V, const int64_t s[3], const int32_t* first, const int32_t* counts, int B, int H_kv, int d,
               const void* K4, const void* V4, const int64_t s4[3], int max_tokens, hipStream_t stream) {
-    if (!K || !V || !counts || !K4 || !V4 || B < 1 || H_kv < 1 || max_tokens < 1) return LC_ERR_INVALID_ARG;
+    if (!counts || !K4 || !V4 || B < 1 || H_kv < 1 || max_tokens < 1) return LC_ERR_INVALID_ARG;
+    int longest = 0;
+    for (int b = 0; b < B; ++b) longest = counts[b] > longest ? counts[b] : longest;
+    if (longest > 0 && (!K || !V)) return LC_ERR_INVALID_ARG;               // (a tensor without rows has no address)
     if (d != LC_HEAD_DIM || H_kv > 65535) return LC_ERR_BAD_SHAPE;
     int rc = check_strides16(s);
     if (rc == LC_OK) rc = lc_check_strides4(s4);

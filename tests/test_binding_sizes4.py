@@ -159,3 +159,21 @@ def test_appending_to_a_cache_that_is_too_small(seen, t):  # noqa: F811
     assert seen == []
     append(_narrow(rows=T), _narrow(rows=T), bf(B, 1, H, 128), bf(B, H, 1, 128))
     assert [name for name, _ in seen] == ["append4"]
+
+
+# ------------------------------------------------------------------ nothing to do
+
+@pytest.mark.parametrize("native", [True, False])
+def test_no_rows_to_store_or_load(native, monkeypatch):
+    """Tensors without rows, which have no address: nothing is launched, no error."""
+    if not native:
+        monkeypatch.setattr(lc, "_fast_mod", lc._Unmarshalled)
+    K, K4 = _wide(rows=0), torch.full((B, H, T, 68), 3, dtype=torch.uint8)
+    for args in (dict(), dict(counts=[0] * B), dict(first=[T, 0, 1], counts=[0] * B)):
+        lc.lc_cache4_store(K, K, K4, K4.clone(), stream=Stream, **args)
+        lc.lc_cache4_load(K4, K4.clone(), K, K, stream=Stream, **args)
+    assert (K4 == 3).all()
+    for bad, code in ((dict(first=[T + 1, 0, 0]), lc.LC_ERR_CAPACITY), (dict(first=[-1, 0, 0]), lc.LC_ERR_INVALID_ARG)):
+        with pytest.raises(lc.LycheeError) as e:
+            lc.lc_cache4_store(K, K, K4, K4.clone(), stream=Stream, **bad)
+        assert e.value.code == code
