@@ -621,7 +621,8 @@ def lc_evict_select(idx: Index, weights, keep_tokens: int, recent_tokens: int, k
     if room:
         _table(weights, True, room[0] * room[1], room[2], "weights")
         _table(keep_lens, False, room[0], 0, "keep_lens")
-    _check(lib().lc_evict_select(idx.handle, _ptr(weights), int(keep_tokens), int(recent_tokens), _ptr(keep_ids), _ptr(keep_bounds),
+    keep, recent = (min(max(int(n), -2 ** 31), 2 ** 31 - 1) for n in (keep_tokens, recent_tokens))       # (as many as there are)
+    _check(lib().lc_evict_select(idx.handle, _ptr(weights), keep, recent, _ptr(keep_ids), _ptr(keep_bounds),
                                  _ptr(keep_counts), _ptr(keep_lens), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)), "lc_evict_select")
 
 

@@ -10,6 +10,7 @@
 
 #include <c10/hip/HIPStream.h>
 
+#include <climits>
 #include <exception>
 #include <initializer_list>
 
@@ -101,7 +102,16 @@ class Args {
         Py_XDECREF(v);
         return r;
     }
-    // The same of an integer alone; a float or a text makes the call not ours (ctypes refuses it).
+    // What int(x) gives, in C's int or the end of its range that is nearest.
+    int limited(int i) {
+        PyObject* const v = PyNumber_Long(a_[i]);
+        int over = 0;
+        const long r = v ? PyLong_AsLongAndOverflow(v, &over) : -1;
+        Py_XDECREF(v);
+        if (over > 0 || r > INT_MAX) return INT_MAX;
+        return over < 0 || r < INT_MIN ? INT_MIN : (int)r;
+    }
+    // integer() of an integer alone; a float or a text makes the call not ours (ctypes refuses it).
     int whole(int i) {
         if (!PyIndex_Check(a_[i])) { foreign_ = true; return -1; }
         PyObject* const v = PyNumber_Index(a_[i]);
@@ -514,7 +524,7 @@ PyObject* evict_select(PyObject*, PyObject* const* args, Py_ssize_t n) {
         const Room room = a.room(10);
         if (!keep_tables(room, ids_t, bounds_t, n_t)) return true;
         if (room.known && (!table(w, true, room.B() * room.H(), room.chunks(), "weights") || !table(lens_t, false, room.B(), 0, "keep_lens"))) return true;
-        const int keep = a.integer(2), recent = a.integer(3);
+        const int keep = a.limited(2), recent = a.limited(3);
         if (PyErr_Occurred()) return false;
         int32_t* const ids = static_cast<int32_t*>(a.ptr(4));
         int32_t* const bounds = static_cast<int32_t*>(a.ptr(5));

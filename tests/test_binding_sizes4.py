@@ -177,3 +177,13 @@ def test_no_rows_to_store_or_load(native, monkeypatch):
         with pytest.raises(lc.LycheeError) as e:
             lc.lc_cache4_store(K, K, K4, K4.clone(), stream=Stream, **bad)
         assert e.value.code == code
+
+
+# ------------------------------------------------------------------ numbers beyond C's int
+
+@pytest.mark.parametrize("given,want", [(2 ** 31 - 1, 2 ** 31 - 1), (2 ** 31, 2 ** 31 - 1), (2 ** 32, 2 ** 31 - 1), (2 ** 40 + 3, 2 ** 31 - 1), (2 ** 80, 2 ** 31 - 1),
+                                        (-1, -1), (-2 ** 32, -2 ** 31), (torch.tensor(9), 9), (7.9, 7)])
+def test_tokens_to_keep_beyond_an_int(seen, t, given, want):  # noqa: F811
+    """To keep 2^32 tokens is to keep them all, not none."""
+    lc.lc_evict_select(Sized, t["weights"], given, given, t["keep"], t["bounds"], t["n"], t["ws"], stream=Stream)
+    assert seen[0][1][2:4] == [want, want]
