@@ -445,6 +445,11 @@ def lc_static_workspace_bytes() -> int:
     return int(lib().lc_static_workspace_bytes())
 
 
+def _close_flags(close_chunk):
+    """A flag for each of the 1024 sequences an append takes at most, as the native module hands them over: those not given are off."""
+    return None if close_chunk is None else (ctypes.c_uint8 * max(1024, len(close_chunk)))(*[1 if c else 0 for c in close_chunk])
+
+
 def lc_append(idx: Index, K, V, k_new, v_new, close_chunk: Optional[Sequence[int]], ws, stream=None) -> None:
     """k_new, v_new bf16 [B][H_kv][d]; close_chunk: host flags per sequence (or None)."""
     rc = (_fast_mod or _fast()).append(idx.address, K, V, k_new, v_new, close_chunk, ws, stream)
@@ -452,9 +457,7 @@ def lc_append(idx: Index, K, V, k_new, v_new, close_chunk: Optional[Sequence[int
         if rc:
             raise LycheeError(rc, "lc_append")
         return
-    cc = None
-    if close_chunk is not None:
-        cc = (ctypes.c_uint8 * len(close_chunk))(*[1 if c else 0 for c in close_chunk])
+    cc = _close_flags(close_chunk)
     assert K.stride() == V.stride()
     rc = lib().lc_append(idx.handle, _ptr(K), _ptr(V), _strides3(K), _ptr(k_new), _ptr(v_new), cc,
                          _ptr(ws), ws.numel() * ws.element_size(), _stream(stream))
@@ -570,9 +573,7 @@ def lc_append4(idx: Index, K4, V4, k_new, v_new, close_chunk: Optional[Sequence[
     room = _room(idx)
     if _done((_fast_mod or _fast()).append4(idx.address, K4, V4, k_new, v_new, close_chunk, stream, room), "lc_append4"):
         return
-    cc = None
-    if close_chunk is not None:
-        cc = (ctypes.c_uint8 * len(close_chunk))(*[1 if c else 0 for c in close_chunk])
+    cc = _close_flags(close_chunk)
     _bfloat16s(k_new, v_new)
     _cache4(K4, V4)
     if room:

@@ -187,3 +187,24 @@ def test_tokens_to_keep_beyond_an_int(seen, t, given, want):  # noqa: F811
     """To keep 2^32 tokens is to keep them all, not none."""
     lc.lc_evict_select(Sized, t["weights"], given, given, t["keep"], t["bounds"], t["n"], t["ws"], stream=Stream)
     assert seen[0][1][2:4] == [want, want]
+
+
+# ------------------------------------------------------------------ close flags
+
+@pytest.mark.parametrize("call", ["lc_append", "lc_append4"])
+def test_fewer_close_flags_than_sequences(t, monkeypatch, call):  # noqa: F811
+    """Without the native module too, the library finds a flag for every sequence it takes; those not given are off."""
+    got = []
+
+    class Library:
+        pass
+    library = Library()
+    setattr(library, call, lambda *a: got.append(bytes(a[6])) or 0)
+    monkeypatch.setattr(lc, "_fast_mod", lc._Unmarshalled)
+    monkeypatch.setattr(lc, "lib", lambda: library)
+    for flags, want in (([1], b"\1"), ([0, 2, True], b"\0\1\1"), ([], b"")):
+        if call == "lc_append":
+            lc.lc_append(Sized, t["K"], t["V"], t["row"], t["row"], flags, t["ws"], stream=Stream)
+        else:
+            lc.lc_append4(Sized, t["K4"], t["V4"], t["row"], t["row"], flags, stream=Stream)
+        assert got.pop() == want + bytes(1024 - len(want))
