@@ -358,6 +358,8 @@ int lc_cache4_load(const void* K4, const void* V4, const int64_t strides4[3], co
  * lc_sparse_decode4 -- lc_sparse_decode over a 4-bit cache: the same list, active set, outputs and workspace.  The rows enter the products as the
  * values they stand for, sums and softmax are float32.  Entries of the list that are no chunk of the sequence hold no tokens.  A token whose
  * logit lies more than 126 powers of two below the largest weighs nothing.
+ * The launch is laid out for the tokens that the handle counts when the call is made (a workgroup for each 128 of the longest sequence at most, as many as
+ * the workspace has room for).  A captured call stays right when the cache has grown, but is split no further: capture it anew when it has doubled.
  */
 int lc_sparse_decode4(const lc_index* idx, const void* q, const void* K4, const void* V4, const int64_t strides4[3],
                       const int32_t* chunk_ids, const int32_t* counts, int cap, int H_q,
@@ -378,7 +380,7 @@ int lc_append4(lc_index* idx, void* K4, void* V4, const int64_t strides4[3], con
  *   weights[b][h][c] += sum over its tokens t and the group's heads g of exp(q_g . k_t / sqrt(d) - lse_g).
  *   chunk_ids, counts, cap   as in lc_sparse_decode, the chunks ascending.  An entry that is no chunk of the sequence is passed over (it holds no tokens in
  *                            lc_sparse_decode4 either), and so is one no larger than a chunk right before it.  In a list that does not ascend otherwise a
- *                            chunk that comes back further on is added to once or twice
+ *                            chunk that comes back further on may be added to more than once
  *   lse        float32 [B][H_q] as lc_sparse_decode or lc_decode_step gave it for the same q; a head with -inf adds nothing
  * The same bits every time, and every chunk added to once, for such lists.  Chunks that are not listed, and the open tail, are not touched.
  */

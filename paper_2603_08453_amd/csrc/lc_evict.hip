@@ -478,6 +478,8 @@ __device__ __forceinline__ void lc_evict_place(int j0, int hi, const int* bnd, i
 // What bounds it is a chain of barriers, LDS atomics and the first loads in one compute unit per sequence: 113 chunks 5.9 us, 4 sequences of 455 6.1, 4096 9.5, 10.9 K 15.7 with the
 // weights' sums before it (4.5; up to 4096 chunks the selecting workgroup makes them, which saves a launch), 4 sequences of 12 K 16.6.  (With the pinned chunks in masks beside the
 // keys, and the range of the keys found here instead of with the sums: 10.9 K 16.9; with the loops over chunks in memory between the others in the code: the first two 6.3 and 6.5.
+// Equal weights are the slow case, and all of the figures are for weights that differ.  With four fifths of the chunks exactly 0 (never listed) and the cut above them 4 sequences of
+// 455 take 5.9 us, 4096 12.6, 10.9 K 24; with the cut among them, where every digit's tokens meet in one word and the ties are scanned, 14, 40 and 86.
 // Digits of the keys from the first bit in which they differ, ranks by a single wavefront and scans of 1024 chunks at a time: 9 us for the first.)
 template <int C, bool FUSED>
 __global__ void __launch_bounds__(LC_EV_THREADS)
@@ -641,7 +643,8 @@ lc_evict_select_kernel(const LcEvictArgs a) {
 // ---- many chunks: several workgroups to a sequence, each with a range of its chunks
 // One alone reads the keys at what a compute unit gets from its L2, and several times.  Three launches behind the keys': the first digit's tokens, added up by all, and by
 // the last one to arrive the cut; the chunks above it, counted, those at it, listed, and by the last one the rest of the search among them; ids and boundaries.
-// Bound by the four launches, each a few trips to memory long: 26 K chunks 24 us (by one workgroup 43), 87 K 28 (142).
+// Bound by the four launches, each a few trips to memory long: 26 K chunks 24 us (by one workgroup 43), 87 K 28 (142).  That is with weights that differ; with four fifths of
+// them 0 and the cut above those 31 and 55, with the cut among them, which the last workgroup alone goes through, 421 and 1257.
 struct LcSlab {
     int lo, hi;           // chunks of this workgroup
     int size;             // of each
