@@ -487,9 +487,10 @@ def _room(idx):
 
 
 def _table(t, floats: bool, rows: int, row: int, name: str) -> None:
-    """t, if there is one, holds `rows` rows of `row` 32-bit numbers one behind the other (row 0: that many numbers, whatever its shape)."""
+    """t, if there is one, holds `rows` rows of `row` 32-bit numbers one behind the other (row 0: that many numbers).  With exactly as many numbers, or
+    a single row, the shape says nothing; of a larger table the rows have to be of that length."""
     assert t is None or (t.is_contiguous() and t.element_size() == 4 and t.is_floating_point() == floats and t.numel() >= rows * (row or 1)
-                         and (row == 0 or t.dim() < 2 or t.shape[-1] == row)), \
+                         and (row == 0 or rows == 1 or t.numel() == rows * row or t.dim() < 2 or t.shape[-1] == row)), \
         f"{name} must be a contiguous {'float32' if floats else 'int32'} table with the index's room"
 
 
@@ -629,14 +630,14 @@ def lc_evict_select(idx: Index, weights, keep_tokens: int, recent_tokens: int, k
 
 def lc_evict_rows(idx: Index, keep_ids, keep_bounds, keep_counts, K, V, K_to, V_to, weights=None, weights_to=None, stream=None) -> None:
     """The kept chunks' rows and the open tail's from K and V to the front of K_to and V_to; bf16 caches, or 4-bit ones (uint8).
-    K_to and V_to: K's shape, with at least max_tokens rows."""
+    K_to and V_to have the index's sequences and heads, and max_tokens rows."""
     room = _room(idx)
     if _done((_fast_mod or _fast()).evict_rows(idx.address, keep_ids, keep_bounds, keep_counts, K, V, K_to, V_to, weights, weights_to, stream, room), "lc_evict_rows"):
         return
     assert K.shape == V.shape and K.stride() == V.stride() and K_to.shape == V_to.shape and K_to.stride() == V_to.stride()
-    assert K.shape[:2] == K_to.shape[:2] and K.shape[3] == K_to.shape[3] and (K.element_size() == 1 or K.shape[3] == LC_HEAD_DIM), "K_to must have K's sequences, heads and row"
-    assert K_to.shape[2] >= (room[3] if room else K.shape[2]) and (room is None or (K.shape[0] >= room[0] and K.shape[1] >= room[1])), \
-        "K_to and V_to must have room for the index's max_tokens rows"
+    B, H, _, rows = room or (K.shape[0], K.shape[1], 0, K.shape[2])
+    assert K.shape[0] >= B and K.shape[1] >= H and K_to.shape[0] >= B and K_to.shape[1] >= H and K_to.shape[2] >= rows and K.shape[3] == K_to.shape[3] \
+        and (K.element_size() == 1 or K.shape[3] == LC_HEAD_DIM), "K_to and V_to must have room for the index's sequences, heads and max_tokens rows like K's"
     _keep_tables(room, keep_ids, keep_bounds, keep_counts)
     if room:
         _table(weights, True, room[0] * room[1], room[2], "weights")

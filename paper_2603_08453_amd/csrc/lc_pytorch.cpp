@@ -387,10 +387,11 @@ PyObject* move4(PyObject*, PyObject* const* args, Py_ssize_t n) {
     });
 }
 
-// Whether t, if there is one, holds `rows` rows of `row` 32-bit numbers one behind the other (row 0: that many numbers, whatever its shape).
+// Whether t, if there is one, holds `rows` rows of `row` 32-bit numbers one behind the other (row 0: that many numbers).  With exactly as many numbers, or a single
+// row, the shape says nothing; of a larger table the rows have to be of that length.
 bool table(const at::Tensor* t, bool floats, int64_t rows, int64_t row, const char* name) {
     if (!t || (t->is_contiguous() && t->element_size() == 4 && t->is_floating_point() == floats && t->numel() >= rows * (row ? row : 1) &&
-               (row == 0 || t->dim() < 2 || t->size(-1) == row)))
+               (row == 0 || rows == 1 || t->numel() == rows * row || t->dim() < 2 || t->size(-1) == row)))
         return true;
     PyErr_Format(PyExc_AssertionError, "%s must be a contiguous %s table with the index's room", name, floats ? "float32" : "int32");
     return false;
@@ -546,9 +547,10 @@ PyObject* evict_select(PyObject*, PyObject* const* args, Py_ssize_t n) {
 
 // Whether every row that an eviction may write lies in the destination (both are caches of four dimensions).
 bool holds_rows(const at::Tensor& K, const at::Tensor& K_to, const Room& room, bool in4) {
-    const bool alike = K.size(0) == K_to.size(0) && K.size(1) == K_to.size(1) && K.size(3) == K_to.size(3) && (in4 || K.size(3) == LC_HEAD_DIM);
-    if (!alike || K_to.size(2) < (room.known ? room.tokens() : K.size(2)) || (room.known && (K.size(0) < room.B() || K.size(1) < room.H()))) {
-        PyErr_SetString(PyExc_AssertionError, "K_to and V_to must have K's sequences, heads and row, and room for the index's max_tokens rows");
+    const int64_t B = room.known ? room.B() : K.size(0), H = room.known ? room.H() : K.size(1), rows = room.known ? room.tokens() : K.size(2);
+    if (K.size(0) < B || K.size(1) < H || K_to.size(0) < B || K_to.size(1) < H || K_to.size(2) < rows || K.size(3) != K_to.size(3) ||
+        (!in4 && K.size(3) != LC_HEAD_DIM)) {
+        PyErr_SetString(PyExc_AssertionError, "K_to and V_to must have room for the index's sequences, heads and max_tokens rows like K's");
         return false;
     }
     return true;

@@ -208,3 +208,26 @@ def test_fewer_close_flags_than_sequences(t, monkeypatch, call):  # noqa: F811
         else:
             lc.lc_append4(Sized, t["K4"], t["V4"], t["row"], t["row"], flags, stream=Stream)
         assert got.pop() == want + bytes(1024 - len(want))
+
+
+# ------------------------------------------------------------------ the same numbers in other shapes
+
+def test_tables_in_other_shapes(seen, t):  # noqa: F811
+    """What lies in memory as the library reads it is taken: heads split into groups, a longer table of a single row."""
+    lc.lc_weigh_chunks(Sized, t["q"], t["K"], t["ids"], t["counts"], t["lse"].reshape(B, H, G), t["weights"].reshape(B * H, M), stream=Stream)
+    lc.lc_sparse_decode4(Sized, t["q"], t["K4"], t["V4"], t["ids"], t["counts"], t["out"].reshape(B, H, G, 128), t["ws"], lse=t["lse"].reshape(B, H, G), stream=Stream)
+
+    class One(Index):
+        sizes = (1, 1, M, T)
+    i32 = lambda *n: torch.zeros(*n, dtype=torch.int32)
+    lc.lc_evict_select(One, torch.zeros(1, 1, 3 * M), 10, 0, i32(1, 2 * M), i32(1, 2 * M + 1), i32(4), t["ws"], stream=Stream)
+    assert [name for name, _ in seen] == ["weigh_chunks", "sparse_decode4", "evict_select"]
+    with pytest.raises(AssertionError):                      # (of several rows a longer one would be read at the wrong places)
+        lc.lc_sparse_decode4(Sized, t["q"], t["K4"], t["V4"], t["ids"], t["counts"], t["out"], t["ws"], lse=torch.zeros(B, H * G + 1), stream=Stream)
+
+
+def test_a_destination_larger_than_the_source(seen, t):  # noqa: F811
+    for index in (Index, Sized):
+        for make in (_wide, _narrow):
+            lc.lc_evict_rows(index, t["keep"], t["bounds"], t["n"], make(), make(), make(b=B + 1, h=H + 1), make(b=B + 1, h=H + 1), stream=Stream)
+    assert [name for name, _ in seen] == ["evict_rows", "evict_rows4"] * 2
